@@ -42,7 +42,8 @@ typedef enum {
     OBC_ERR_CAPACITY = -8      /* the problem exceeds the fixed capacity of an allocation-free entry point */
 } obc_status;
 
-typedef enum { OBC_F32 = 0, OBC_BF16 = 1 } obc_dtype;
+/* OBC_E4M3 (8 bits: sign, 4 exponent bits, 3 of mantissa, largest value 448) only for the pages of a paged cache */
+typedef enum { OBC_F32 = 0, OBC_BF16 = 1, OBC_E4M3 = 2 } obc_dtype;
 
 /* score variants (bitmask).  The scores buffer holds one [B,Hkv,max_len] fp32 plane per set bit,
  * in ascending bit order (V, K, VK, ATTN, VATP). */
@@ -336,6 +337,85 @@ obc_status obc_decode_step(const obc_decode_params* p, obc_tensor q_t, obc_tenso
                            obc_tensor k_cache, obc_tensor v_cache, float* s_acc, int32_t* pos,
                            int32_t* state, int32_t step_pos,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Paged caches.  The K and V rows of a KV list live in pages of page_size tokens out of a pool; a list is the
+ * sequence of page numbers in its row of `table`, of which the first ceil(len / page_size) count.  Lists belong to
+ * a batch item (table_stride_h = lens_stride_h = 0: a page holds the rows of all KV heads), or to a (batch item,
+ * KV head), as after an eviction with budgets per head (pages may then hold one head each: k.stride_h =
+ * v.stride_h = scale_stride_h = 0).
+ *   types   fp32, bf16, or e4m3 with a scale per row: x = code * 2^(scale - 127).  obc_paged_write takes the smallest
+ *           power of two for which max |x| <= 448 scales (never below 2^-126; the division is then exact and every
+ *           value is rounded once, to nearest, ties to even).  A row that holds an infinity or a NaN is stored with
+ *           scale 255 and reads as NaN.
+ *   bounds  lengths and page numbers are read on the device only.  A length counts as if clamped to
+ *           [0, max_pages * page_size].  A page number outside [0, n_pages) reads as rows of zeros and is never
+ *           written.  Rows of a page behind a list's end may hold anything, NaN among it, and stay as they are.
+ *   sharing several lists may name the same page (a common prefix) as long as none of them writes it.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    size_t struct_size;
+    obc_tensor k, v;           /* [n_pages, n_kv_heads or 1, page_size, d]: stride_b goes from page to page */
+    uint8_t* k_scale;          /* device, e4m3 only (else NULL): biased exponents, tokens of a page contiguous */
+    uint8_t* v_scale;
+    int64_t scale_stride_p, scale_stride_h;   /* from page to page, from head to head; multiples of 8 */
+    int32_t batch, n_kv_heads, head_dim;
+    int32_t n_pages, page_size;               /* page_size: a multiple of 8 */
+    int32_t max_pages;                        /* page numbers in a row of table */
+    const int32_t* table;                     /* device */
+    int64_t table_stride_b, table_stride_h;
+    const int32_t* lens;                      /* device: tokens of every list */
+    int64_t lens_stride_b, lens_stride_h;
+} obc_pages;
+
+/*
+ * obc_paged_write: appends rows to the lists, rounding them to the pages' type on the way.  `lens` is the length AFTER
+ * the call: of the n rows that a list receives, row j goes to token len - n + j (rows that would land before token 0, or on
+ * a page that is not there, are dropped).  Row j of list (b, h) is k[b,h,j] or, with idx, k[b,h,idx[b,h,j]] (what
+ * obc_select returned: the kept rows move into pages in one pass; entries outside [0, src_tokens) leave
+ * their token's place as it is).  k, v: f32 or bf16, one type.  Pages that receive rows must belong to one list.
+ */
+typedef struct {
+    size_t struct_size;
+    int32_t rows;              /* rows per list in this call: entries of idx, or tokens of k and v to take */
+    int32_t src_tokens;        /* token extent of k and v */
+    const int32_t* new_lens;   /* device: n of every list (clamped to [0, rows]); NULL: all `rows` */
+    int64_t new_lens_stride_b, new_lens_stride_h;
+    const int32_t* idx;        /* device [batch, n_kv_heads, rows] or NULL */
+} obc_paged_write_params;
+obc_status obc_paged_write(const obc_pages* c, const obc_paged_write_params* p, obc_tensor k, obc_tensor v, void* stream);
+
+/*
+ * obc_paged_read: the lists as dense caches, in the layout obc_score and obc_compact take: k_out, v_out [B,Hkv,n_tokens,d], f32 or
+ * bf16 (one type).  Rows [0, min(len, n_tokens)) are written; the rows behind them are left as they are, or set
+ * to zero with zero_rows != 0.
+ */
+obc_status obc_paged_read(const obc_pages* c, int32_t n_tokens, obc_tensor k_out, obc_tensor v_out, int32_t zero_rows, void* stream);
+
+/*
+ * obc_paged_attention: attention of a chunk of new tokens (one token when decoding) over the lists.  The new tokens' own
+ * rows are in the cache already (obc_paged_write), as the last q_len tokens of their lists.  Query i = 0..q_len-1 of batch item b
+ * sees the tokens p <= len - q_len + i of its KV head's list (all p < len unless causal):
+ *   Z_ip = scale * q_i . k_p;   lse_i = log sum_p exp Z_ip;   o_i = sum_p exp(Z_ip - lse_i) v_p
+ * A query that sees nothing has o = 0 and lse = -inf.  o and lse are what obc_score_given takes.
+ *   q, o   [B,Hq,n_tokens,d], one type: f32 over f32 pages, bf16 over bf16 or e4m3 pages
+ *   lse    device fp32 [B,Hq,n_tokens] contiguous, or NULL
+ * Rows i >= q_len of o and lse are left as they are.  Sums and softmax statistics are fp32.  Infinities and NaN are no
+ * different from any value in a row that a query sees, and reach no query that does not see them.  e4m3 scales
+ * above 186 (rows of more than 1e20) count as NaN.
+ * A device-side wait that gives up raises the workspace's status word: obc_score_status() reads it.
+ */
+typedef struct {
+    size_t struct_size;
+    int32_t n_q_heads;
+    int32_t n_tokens;          /* T: query rows per head in q and o */
+    const int32_t* q_lens;     /* device [batch] (clamped to [0, n_tokens]), or NULL: all n_tokens */
+    float scale;               /* <= 0 selects 1/sqrt(head_dim) */
+    int32_t causal;
+} obc_attention_params;
+obc_status obc_paged_attention_workspace(const obc_pages* c, const obc_attention_params* p, size_t* bytes /* host out */);
+obc_status obc_paged_attention(const obc_pages* c, const obc_attention_params* p, obc_tensor q, obc_tensor o, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Optional per-kernel timing, used by the benchmark (no counterpart in the paper).  Between

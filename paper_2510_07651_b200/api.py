@@ -10,13 +10,14 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libobcache.so")
 
-OBC_F32, OBC_BF16 = 0, 1
+OBC_F32, OBC_BF16, OBC_E4M3 = 0, 1, 2
 OBC_VAR_V, OBC_VAR_K, OBC_VAR_VK, OBC_VAR_ATTN, OBC_VAR_VATP = 1, 2, 4, 8, 16
 OBC_POOL_NONE, OBC_POOL_AVG, OBC_POOL_MAX = 0, 1, 2
 OBC_PATH_AUTO, OBC_PATH_SIMT, OBC_PATH_TC = 0, 1, 2
@@ -26,7 +27,8 @@ PATHS = {"auto": OBC_PATH_AUTO, "simt": OBC_PATH_SIMT, "tc": OBC_PATH_TC}
 
 EXPORTS = ["obc_score_workspace", "obc_score", "obc_score_given", "obc_window_attention", "obc_merge_attention", "obc_shard_indices", "obc_score_status", "obc_score_kernel_spans", "obc_select_workspace", "obc_select",
            "obc_select_noalloc", "obc_select_adaptive_workspace", "obc_select_adaptive", "obc_compact", "obc_compact_padded",
-           "obc_decode_workspace", "obc_decode_step", "obc_profile_begin", "obc_profile_end",
+           "obc_decode_workspace", "obc_decode_step", "obc_paged_write", "obc_paged_read", "obc_paged_attention_workspace",
+           "obc_paged_attention", "obc_profile_begin", "obc_profile_end",
            "obc_status_string", "obc_last_cuda_error", "obc_version"]
 
 
@@ -65,6 +67,24 @@ class obc_decode_params(C.Structure):
                 ("variant", C.c_uint32), ("scale", C.c_float), ("acc_window", C.c_int32), ("s_hist", C.c_void_p)]
 
 
+class obc_pages(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("k", obc_tensor), ("v", obc_tensor), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("scale_stride_p", C.c_int64), ("scale_stride_h", C.c_int64), ("batch", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32),
+                ("table", C.c_void_p), ("table_stride_b", C.c_int64), ("table_stride_h", C.c_int64),
+                ("lens", C.c_void_p), ("lens_stride_b", C.c_int64), ("lens_stride_h", C.c_int64)]
+
+
+class obc_paged_write_params(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("rows", C.c_int32), ("src_tokens", C.c_int32), ("new_lens", C.c_void_p),
+                ("new_lens_stride_b", C.c_int64), ("new_lens_stride_h", C.c_int64), ("idx", C.c_void_p)]
+
+
+class obc_attention_params(C.Structure):
+    _fields_ = [("struct_size", C.c_size_t), ("n_q_heads", C.c_int32), ("n_tokens", C.c_int32), ("q_lens", C.c_void_p),
+                ("scale", C.c_float), ("causal", C.c_int32)]
+
+
 class obc_kernel_time(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("launches", C.c_int32), ("ms_total", C.c_float)]
 
@@ -98,6 +118,10 @@ def lib():
         L.obc_compact_padded.argtypes = [C.c_int32] * 5 + [obc_tensor, obc_tensor, vp, obc_tensor, obc_tensor, vp, vp, C.c_uint32, vp]
         L.obc_decode_workspace.argtypes = [C.POINTER(obc_decode_params), sz]
         L.obc_decode_step.argtypes = [C.POINTER(obc_decode_params)] + [obc_tensor] * 5 + [vp, vp, vp, C.c_int32, vp, C.c_size_t, vp]
+        L.obc_paged_write.argtypes = [C.POINTER(obc_pages), C.POINTER(obc_paged_write_params), obc_tensor, obc_tensor, vp]
+        L.obc_paged_read.argtypes = [C.POINTER(obc_pages), C.c_int32, obc_tensor, obc_tensor, C.c_int32, vp]
+        L.obc_paged_attention_workspace.argtypes = [C.POINTER(obc_pages), C.POINTER(obc_attention_params), sz]
+        L.obc_paged_attention.argtypes = [C.POINTER(obc_pages), C.POINTER(obc_attention_params), obc_tensor, obc_tensor, vp, vp, C.c_size_t, vp]
         L.obc_profile_begin.argtypes = []
         L.obc_profile_end.argtypes = [C.POINTER(obc_kernel_time), C.c_int32, C.POINTER(C.c_int32)]
         L.obc_status_string.argtypes = [C.c_int]
@@ -348,6 +372,54 @@ def obc_decode_step(q_t, k_t, v_t, k_cache, v_cache, s_acc, pos, state, step_pos
                                          int(acc_window), s_hist), "obc_decode_step")
 
 
+class PagedCache(NamedTuple):
+    """A paged KV cache (see include/obcache.h): views of the caller's tensors, nothing of its own.
+
+    k, v               [n_pages, Hkv, page_size, d] float32, bfloat16 or float8_e4m3fn; [n_pages, 1, page_size, d] where `table`
+                       has a list per head
+    table              int32 [B, max_pages] page numbers, or [B, Hkv, max_pages]
+    lens               int32 [B] or [B, Hkv]: tokens of every list
+    k_scale, v_scale   uint8 [n_pages, heads, page_size] with float8 pages: a row is its codes times 2^(scale - 127)
+    """
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+def obc_paged_write(cache: PagedCache, k, v, *, new_lens=None, idx=None) -> None:
+    """Append rows to the lists (quantised on the way into float8 pages).  cache.lens holds the lengths after the call: list
+    (b, h) receives its last n = new_lens[b] (or [b, h]; default: all) tokens from k, v [B,Hkv,T,d], rows 0..n-1, or with
+    idx int32 [B,Hkv,S] (the selection's result) the rows it names."""
+    _result(_native().paged_write(*cache, k, v, new_lens, idx) or None, "obc_paged_write")
+
+
+def obc_paged_read(cache: PagedCache, *, n_tokens=None, dtype=None, k_out=None, v_out=None):
+    """The lists as dense caches (k, v) [B,Hkv,n_tokens,d], float32 or bfloat16.  Given outputs keep what they hold behind a list's end;
+    outputs made here (n_tokens: default all that the table can hold) hold zeros there."""
+    if n_tokens is None:
+        n_tokens = cache.table.shape[-1] * cache.k.shape[2]
+    if dtype is None:
+        dtype = torch.float32 if cache.k.dtype == torch.float32 else torch.bfloat16
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported dtype {dtype}")
+    return _result(_native().paged_read(*cache, int(n_tokens), 1 if dtype == torch.float32 else 0, k_out, v_out), "obc_paged_read")
+
+
+def obc_paged_attention_workspace(q, cache: PagedCache) -> int:
+    n = _native().paged_attention(*cache, q, None, 0.0, -1, None, None, None)
+    _check(min(n, 0), "obc_paged_attention_workspace")
+    return n
+
+
+def obc_paged_attention(q, cache: PagedCache, *, q_lens=None, scale=0.0, causal=True, o=None, lse=None, workspace=None):
+    """Attention of new tokens q [B,Hq,T,d], the last q_lens[b] (default T) tokens of their lists, over a paged cache that holds their rows
+    already: (o like q, lse fp32 [B,Hq,T], natural log), as obc_score_given takes them.  Rows behind q_lens are left as they are."""
+    return _result(_native().paged_attention(*cache, q, q_lens, scale, 1 if causal else 0, o, lse, workspace), "obc_paged_attention")
+
+
 def obc_profile_begin():
     """Start bracketing every library kernel with CUDA events (benchmark use)."""
     _check(lib().obc_profile_begin(), "obc_profile_begin")
@@ -377,3 +449,26 @@ def evict_prefill(q, k, v, *, budget=0, budgets=None, seq_lens=None, variant="VK
                      n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel)
     k_out, v_out = obc_compact(k, v, idx)
     return k_out, v_out, idx, scores
+
+
+def evict_to_pages(q, k, v, cache: PagedCache, *, budget, seq_lens=None, variant="VK", n_sink=0, n_recent=None, pool="none",
+                   pool_kernel=1, causal=True, path="auto", safeguard=None):
+    """The prefill hot path into pages: score -> pool/select -> the kept rows of k, v, quantised if need be, into the lists of `cache`, which
+    become the whole lists: cache.lens is set.  With `safeguard` the budgets are head-adaptive and cache.lens is int32
+    [B,Hkv], contiguous (a head may keep as many tokens as its list's pages hold).  Returns (idx, scores)."""
+    n_recent = q.shape[2] if n_recent is None else n_recent
+    scores = obc_score(q, k, v, seq_lens=seq_lens, causal=causal, variants=(variant,), path=path)
+    room = cache.table.shape[-1] * cache.k.shape[2]
+    if safeguard is None:
+        if budget > room:
+            raise ValueError("the lists' pages do not hold the budget")
+        idx = obc_select(scores[0], budget=budget, seq_lens=seq_lens, n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel)
+        cache.lens.fill_(budget)
+        obc_paged_write(cache, k, v, idx=idx)
+    else:
+        if cache.lens.dim() != 2 or not cache.lens.is_contiguous() or (cache.table.dim() != 3 and cache.k.shape[1] > 1):
+            raise ValueError("head-adaptive budgets need a list per head: lens [B,Hkv], table [B,Hkv,max_pages]")
+        idx, _ = obc_select_adaptive(scores[0], budget=budget, safeguard=safeguard, idx_stride=min(room, k.shape[2]), seq_lens=seq_lens,
+                                     n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel, counts=cache.lens)
+        obc_paged_write(cache, k, v, new_lens=cache.lens, idx=idx)
+    return idx, scores

@@ -387,6 +387,107 @@ obc_status obc_decode_step(const obc_decode_params* p, obc_tensor q_t, obc_tenso
                          step_pos, workspace, (cudaStream_t)stream);
 }
 
+// ---- paged caches --------------------------------------------------------------------------------
+static obc_status check_pages_tensor(const obc_tensor& t, int dtype) {
+    if (!t.ptr) return OBC_ERR_NULL;
+    if (t.dtype != dtype) return OBC_ERR_UNSUPPORTED;
+    const long long es = dtype == OBC_E4M3 ? 1 : elem_size(dtype);
+    if (((uintptr_t)t.ptr & 15) != 0 || (t.stride_t * es) % 16 || (t.stride_h * es) % 16 || (t.stride_b * es) % 16) return OBC_ERR_ALIGN;
+    // a bulk copy's descriptor holds strides below 2^40 bytes
+    if (t.stride_t < kD || t.stride_h < 0 || t.stride_b < 0 || t.stride_t * es >= 1ll << 40 || t.stride_h * es >= 1ll << 40 || t.stride_b * es >= 1ll << 40)
+        return OBC_ERR_SHAPE;
+    return OBC_OK;
+}
+
+static obc_status resolve_pages(const obc_pages* c, PagesView* v) {
+    if (!c) return OBC_ERR_NULL;
+    if (c->struct_size != sizeof(obc_pages)) return OBC_ERR_UNSUPPORTED;
+    if (c->head_dim != kD) return OBC_ERR_UNSUPPORTED;
+    if (c->batch < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->page_size < 8 || c->page_size % 8 || c->max_pages < 1) return OBC_ERR_SHAPE;
+    if ((long long)c->batch * c->n_kv_heads > 65535 || (long long)c->max_pages * c->page_size > 0x7fff0000LL) return OBC_ERR_SHAPE;
+    if (!c->table || !c->lens) return OBC_ERR_NULL;
+    if ((((uintptr_t)c->table | (uintptr_t)c->lens) & 3) != 0) return OBC_ERR_ALIGN;
+    if (c->table_stride_b < 0 || c->table_stride_h < 0 || c->lens_stride_b < 0 || c->lens_stride_h < 0) return OBC_ERR_SHAPE;
+    const int dtype = c->k.dtype;
+    if (dtype != OBC_F32 && dtype != OBC_BF16 && dtype != OBC_E4M3) return OBC_ERR_UNSUPPORTED;
+    obc_status st;
+    if ((st = check_pages_tensor(c->k, dtype)) != OBC_OK) return st;
+    if ((st = check_pages_tensor(c->v, dtype)) != OBC_OK) return st;
+    if (c->n_kv_heads > 1 && (c->k.stride_h == 0) != (c->v.stride_h == 0)) return OBC_ERR_SHAPE;
+    if ((dtype == OBC_E4M3) != (c->k_scale != nullptr) || (dtype == OBC_E4M3) != (c->v_scale != nullptr)) return dtype == OBC_E4M3 ? OBC_ERR_NULL : OBC_ERR_UNSUPPORTED;
+    if (dtype == OBC_E4M3) {
+        if ((((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 7) != 0 || c->scale_stride_p % 8 || c->scale_stride_h % 8) return OBC_ERR_ALIGN;
+        if (c->scale_stride_p < 0 || c->scale_stride_h < 0) return OBC_ERR_SHAPE;
+    }
+    *v = PagesView{c->batch, c->n_kv_heads, c->n_pages, c->page_size, c->max_pages, c->max_pages * c->page_size, dtype,
+                   view(c->k), view(c->v), c->k_scale, c->v_scale, c->scale_stride_p, c->scale_stride_h,
+                   c->table, c->table_stride_b, c->table_stride_h, c->lens, c->lens_stride_b, c->lens_stride_h};
+    return OBC_OK;
+}
+
+obc_status obc_paged_write(const obc_pages* c, const obc_paged_write_params* p, obc_tensor k, obc_tensor v, void* stream) {
+    PagesView pv;
+    obc_status st = resolve_pages(c, &pv);
+    if (st != OBC_OK) return st;
+    if (!p) return OBC_ERR_NULL;
+    if (p->struct_size != sizeof(obc_paged_write_params)) return OBC_ERR_UNSUPPORTED;
+    if (p->rows < 1 || p->src_tokens < 1 || (!p->idx && p->rows > p->src_tokens)) return OBC_ERR_SHAPE;
+    if (p->new_lens_stride_b < 0 || p->new_lens_stride_h < 0) return OBC_ERR_SHAPE;
+    if ((((uintptr_t)p->new_lens | (uintptr_t)p->idx) & 3) != 0) return OBC_ERR_ALIGN;
+    if ((st = check_tensor(k, true)) != OBC_OK) return st;
+    if ((st = check_tensor(v, true)) != OBC_OK) return st;
+    if (k.dtype != v.dtype) return OBC_ERR_UNSUPPORTED;
+    const PagedWrite w{p->rows, p->src_tokens, k.dtype, p->new_lens, p->new_lens_stride_b, p->new_lens_stride_h, p->idx};
+    return launch_paged_write(pv, w, view(k), view(v), (cudaStream_t)stream);
+}
+
+obc_status obc_paged_read(const obc_pages* c, int32_t n_tokens, obc_tensor k_out, obc_tensor v_out, int32_t zero_rows, void* stream) {
+    PagesView pv;
+    obc_status st = resolve_pages(c, &pv);
+    if (st != OBC_OK) return st;
+    if (n_tokens < 1) return OBC_ERR_SHAPE;
+    if ((st = check_tensor(k_out, true)) != OBC_OK) return st;
+    if ((st = check_tensor(v_out, true)) != OBC_OK) return st;
+    if (k_out.dtype != v_out.dtype) return OBC_ERR_UNSUPPORTED;
+    return launch_paged_read(pv, n_tokens, k_out.dtype, view(k_out), view(v_out), zero_rows != 0, (cudaStream_t)stream);
+}
+
+static obc_status resolve_attention(const obc_pages* c, const obc_attention_params* p, PagesView* pv, AttnShape* s) {
+    obc_status st = resolve_pages(c, pv);
+    if (st != OBC_OK) return st;
+    if (!p) return OBC_ERR_NULL;
+    if (p->struct_size != sizeof(obc_attention_params)) return OBC_ERR_UNSUPPORTED;
+    if (p->n_q_heads < 1 || p->n_q_heads % c->n_kv_heads || p->n_tokens < 1) return OBC_ERR_SHAPE;
+    if (((uintptr_t)p->q_lens & 3) != 0) return OBC_ERR_ALIGN;
+    *s = AttnShape{p->n_q_heads, p->n_q_heads / c->n_kv_heads, p->n_tokens, p->q_lens, p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)kD), p->causal != 0};
+    // rows of all lists, padded to the smallest tile, are counted in 32 bits
+    if ((long long)c->batch * c->n_kv_heads * (((long long)s->G * s->T + 15) / 16 * 16) > 0x7fffffffLL) return OBC_ERR_SHAPE;
+    return OBC_OK;
+}
+
+obc_status obc_paged_attention_workspace(const obc_pages* c, const obc_attention_params* p, size_t* bytes) {
+    if (!bytes) return OBC_ERR_NULL;
+    PagesView pv; AttnShape s;
+    const obc_status st = resolve_attention(c, p, &pv, &s);
+    if (st != OBC_OK) return st;
+    *bytes = paged_attention_bytes(pv, s);
+    return OBC_OK;
+}
+
+obc_status obc_paged_attention(const obc_pages* c, const obc_attention_params* p, obc_tensor q, obc_tensor o, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    PagesView pv; AttnShape s;
+    obc_status st = resolve_attention(c, p, &pv, &s);
+    if (st != OBC_OK) return st;
+    if ((st = check_tensor(q, true)) != OBC_OK) return st;
+    if ((st = check_tensor(o, true)) != OBC_OK) return st;
+    if (q.dtype != o.dtype || (q.dtype == OBC_F32) != (pv.dtype == OBC_F32)) return OBC_ERR_UNSUPPORTED;
+    if (((uintptr_t)lse & 3) != 0) return OBC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < paged_attention_bytes(pv, s)) return OBC_ERR_WORKSPACE;
+    if (((uintptr_t)workspace & 255) != 0) return OBC_ERR_ALIGN;
+    return launch_paged_attention(pv, s, view(q), view(o), lse, workspace, (cudaStream_t)stream);
+}
+
 obc_status obc_profile_begin(void) {
     std::lock_guard<std::mutex> lk(g_prof_mu);
     for (auto& r : g_prof) { cudaEventDestroy(r.e0); cudaEventDestroy(r.e1); }

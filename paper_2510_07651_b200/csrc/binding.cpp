@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -289,9 +290,173 @@ PyObject* n_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- paged caches ------------------------------------------------------------------------------------
+bool bad(const char* what) { PyErr_SetString(PyExc_ValueError, what); return false; }
+
+// The six tensors of a PagedCache, from a[0] on: k, v, table, lens, k_scale, v_scale.
+struct PagesArg { const Tensor *k, *v, *table, *lens, *ks, *vs; obc_pages c; };
+bool pages_arg(PyObject* const* a, PagesArg* g) {
+    if (!tensor_arg(a[0], &g->k) || !tensor_arg(a[1], &g->v) || !tensor_arg(a[2], &g->table) || !tensor_arg(a[3], &g->lens) ||
+        !tensor_arg(a[4], &g->ks, true) || !tensor_arg(a[5], &g->vs, true)) return false;
+    const Tensor &k = *g->k, &v = *g->v, &table = *g->table, &lens = *g->lens, &ks = *g->ks, &vs = *g->vs;
+    if (!k.is_cuda() || k.dim() != 4 || k.stride(3) != 1 || !v.is_cuda() || v.dim() != 4 || v.stride(3) != 1 || v.sizes() != k.sizes())
+        return bad("expected CUDA pages k, v [n_pages, heads, page_size, head_dim] of one shape, with contiguous head_dim");
+    const auto st = k.scalar_type();
+    if (v.scalar_type() != st || (st != at::kFloat && st != at::kBFloat16 && st != at::kFloat8_e4m3fn)) {
+        PyErr_SetString(PyExc_TypeError, "pages are float32, bfloat16 or float8_e4m3fn, k and v alike");
+        return false;
+    }
+    if (table.scalar_type() != at::kInt || (table.dim() != 2 && table.dim() != 3) || (table.size(-1) > 1 && table.stride(-1) != 1))
+        return bad("table must be an int32 tensor [batch, max_pages] or [batch, heads, max_pages] with contiguous page numbers");
+    const int64_t B = table.size(0), H = table.dim() == 3 ? table.size(1) : k.size(1);
+    const bool one_head = table.dim() == 3 && k.size(1) == 1;
+    if (!one_head && k.size(1) != H) return bad("pages hold the rows of all KV heads, or (table with a list per head) of one");
+    if (lens.scalar_type() != at::kInt || (lens.dim() == 1 ? lens.size(0) != B : lens.dim() != 2 || lens.size(0) != B || lens.size(1) != H))
+        return bad("lens must be an int32 tensor [batch] or [batch, heads]");
+    const bool e4m3 = st == at::kFloat8_e4m3fn;
+    if (e4m3 != ks.defined() || e4m3 != vs.defined()) return bad("k_scale and v_scale go with float8_e4m3fn pages");
+    if (e4m3)
+        for (const Tensor* s : {&ks, &vs})
+            if (s->scalar_type() != at::kByte || s->sizes() != k.sizes().slice(0, 3) || s->stride(2) != 1 || s->strides() != ks.strides())
+                return bad("k_scale and v_scale must be uint8 tensors [n_pages, heads, page_size], laid out alike, with contiguous tokens");
+    for (const Tensor* t : {g->v, g->table, g->lens, g->ks, g->vs})
+        if (t->defined() && t->device() != k.device()) return bad("the tensors of a paged cache must be on one device");
+    for (int64_t n : {k.size(0), k.size(2), table.size(-1), B, H})
+        if (n > 0x7fffffff) return bad("a paged cache's extents must fit 32 bits");
+    obc_pages& c = g->c;
+    c = obc_pages{};
+    c.struct_size = sizeof(c);
+    const int dt = e4m3 ? OBC_E4M3 : st == at::kFloat ? OBC_F32 : OBC_BF16;
+    c.k = obc_tensor{k.data_ptr(), dt, k.stride(0), one_head ? 0 : k.stride(1), k.stride(2)};
+    c.v = obc_tensor{v.data_ptr(), dt, v.stride(0), one_head ? 0 : v.stride(1), v.stride(2)};
+    if (e4m3) {
+        c.k_scale = ptr<uint8_t>(ks); c.v_scale = ptr<uint8_t>(vs);
+        c.scale_stride_p = ks.stride(0); c.scale_stride_h = one_head ? 0 : ks.stride(1);
+    }
+    c.batch = (int32_t)B; c.n_kv_heads = (int32_t)H; c.head_dim = (int32_t)k.size(3);
+    c.n_pages = (int32_t)k.size(0); c.page_size = (int32_t)k.size(2); c.max_pages = (int32_t)table.size(-1);
+    c.table = ptr<int32_t>(table); c.table_stride_b = table.stride(0); c.table_stride_h = table.dim() == 3 ? table.stride(1) : 0;
+    c.lens = ptr<int32_t>(lens); c.lens_stride_b = lens.stride(0); c.lens_stride_h = lens.dim() == 2 ? lens.stride(1) : 0;
+    return true;
+}
+bool on_device(const PagesArg& g, std::initializer_list<const Tensor*> ts) {
+    for (const Tensor* t : ts)
+        if (t->defined() && t->device() != g.k->device()) return bad("all tensors must be on the pages' device");
+    return true;
+}
+void* stream_of(const PagesArg& g) { return c10::cuda::getCurrentCUDAStream(g.k->device().index()).stream(); }
+
+// paged_write(k, v, table, lens, k_scale, v_scale, new_k, new_v, new_lens, idx) -> None
+PyObject* n_paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!expect(n, 10)) return nullptr;
+    PagesArg g;
+    const Tensor *nk, *nv, *lens, *idx;
+    obc_tensor tk, tv;
+    if (!pages_arg(a, &g) || !view4_arg(a[6], &nk, &tk) || !view4_arg(a[7], &nv, &tv) || !tensor_arg(a[8], &lens, true) || !tensor_arg(a[9], &idx, true) ||
+        !on_device(g, {nk, nv, lens, idx})) return nullptr;
+    const int64_t B = g.c.batch, H = g.c.n_kv_heads;
+    if (nk->size(0) != B || nk->size(1) != H || nk->size(3) != g.k->size(3) || nv->sizes() != nk->sizes()) { bad("k and v must be [batch, heads, tokens, head_dim] like the lists"); return nullptr; }
+    if (lens->defined() && (lens->scalar_type() != at::kInt || (lens->dim() == 1 ? lens->size(0) != B : lens->dim() != 2 || lens->size(0) != B || lens->size(1) != H))) {
+        bad("new_lens must be an int32 tensor [batch] or [batch, heads]");
+        return nullptr;
+    }
+    if (idx->defined() && (idx->scalar_type() != at::kInt || idx->dim() != 3 || idx->size(0) != B || idx->size(1) != H || !idx->is_contiguous())) {
+        bad("idx must be a contiguous int32 tensor [batch, heads, rows]");
+        return nullptr;
+    }
+    obc_paged_write_params p{};
+    p.struct_size = sizeof(p);
+    p.src_tokens = (int32_t)nk->size(2); p.rows = idx->defined() ? (int32_t)idx->size(2) : p.src_tokens;
+    p.new_lens = ptr<int32_t>(*lens);
+    if (lens->defined()) { p.new_lens_stride_b = lens->stride(0); p.new_lens_stride_h = lens->dim() == 2 ? lens->stride(1) : 0; }
+    p.idx = ptr<int32_t>(*idx);
+    const c10::cuda::CUDAGuard guard(g.k->device());
+    void* s = stream_of(g);
+    return status(unlocked([&] { return obc_paged_write(&g.c, &p, tk, tv, s); }));
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_read(k, v, table, lens, k_scale, v_scale, n_tokens, f32, k_out, v_out) -> (k_out, v_out); outputs made here have zeros behind the lists
+PyObject* n_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!expect(n, 10)) return nullptr;
+    PagesArg g;
+    const Tensor *ko, *vo;
+    if (!pages_arg(a, &g) || !tensor_arg(a[8], &ko, true) || !tensor_arg(a[9], &vo, true) || !on_device(g, {ko, vo})) return nullptr;
+    const long n_tokens = as_long(a[6]), f32 = as_long(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    Tensor k_out = *ko, v_out = *vo;
+    const bool mine = !k_out.defined();
+    if (mine != !v_out.defined()) { bad("give both outputs or neither"); return nullptr; }
+    if (mine) {
+        if (n_tokens < 1) return status(OBC_ERR_SHAPE);
+        const auto opt = g.k->options().dtype(f32 ? at::kFloat : at::kBFloat16);
+        k_out = at::empty({g.c.batch, g.c.n_kv_heads, n_tokens, g.k->size(3)}, opt);
+        v_out = at::empty_like(k_out);
+    }
+    obc_tensor tk, tv;
+    if (!view4(k_out, &tk) || !view4(v_out, &tv)) return nullptr;
+    if (k_out.size(0) != g.c.batch || k_out.size(1) != g.c.n_kv_heads || k_out.size(3) != g.k->size(3) || v_out.sizes() != k_out.sizes()) {
+        bad("k_out and v_out must be [batch, heads, tokens, head_dim] like the lists");
+        return nullptr;
+    }
+    const c10::cuda::CUDAGuard guard(g.k->device());
+    void* s = stream_of(g);
+    const obc_status st = unlocked([&] { return obc_paged_read(&g.c, (int32_t)k_out.size(2), tk, tv, mine ? 1 : 0, s); });
+    return st == OBC_OK ? tuple_of({k_out, v_out}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// paged_attention(k, v, table, lens, k_scale, v_scale, q, q_lens, scale, causal, o, lse, workspace) -> (o, lse);
+// causal < 0: the workspace's size in bytes
+PyObject* n_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!expect(n, 13)) return nullptr;
+    PagesArg g;
+    const Tensor *q, *q_lens, *o_in, *lse_in, *ws_in;
+    obc_tensor tq, to;
+    if (!pages_arg(a, &g) || !view4_arg(a[6], &q, &tq) || !tensor_arg(a[7], &q_lens, true) || !tensor_arg(a[10], &o_in, true) ||
+        !tensor_arg(a[11], &lse_in, true) || !tensor_arg(a[12], &ws_in, true) || !on_device(g, {q, q_lens, o_in, lse_in, ws_in})) return nullptr;
+    const double scale = PyFloat_AsDouble(a[8]);
+    const long causal = as_long(a[9]);
+    if (PyErr_Occurred()) return nullptr;
+    if (q->size(0) != g.c.batch || q->size(3) != g.k->size(3)) { bad("q must be [batch, query heads, tokens, head_dim]"); return nullptr; }
+    if (q_lens->defined() && (q_lens->scalar_type() != at::kInt || q_lens->dim() != 1 || q_lens->size(0) != g.c.batch || !q_lens->is_contiguous())) {
+        bad("q_lens must be a contiguous int32 tensor [batch]");
+        return nullptr;
+    }
+    obc_attention_params p{};
+    p.struct_size = sizeof(p);
+    p.n_q_heads = (int32_t)q->size(1); p.n_tokens = (int32_t)q->size(2); p.q_lens = ptr<int32_t>(*q_lens);
+    p.scale = (float)scale; p.causal = causal != 0;
+    const c10::cuda::CUDAGuard guard(g.k->device());
+    size_t need = 0;
+    if (causal < 0 || !ws_in->defined()) {
+        const obc_status st = obc_paged_attention_workspace(&g.c, &p, &need);
+        if (causal < 0) return st == OBC_OK ? PyLong_FromSize_t(need) : PyLong_FromLong((long)st);
+        if (st != OBC_OK) return status(st);
+    }
+    if (ws_in->defined() && !ws_in->is_contiguous()) { bad("workspace must be contiguous"); return nullptr; }
+    const Tensor ws = ws_in->defined() ? *ws_in : bytes_like(need, *g.k);
+    const Tensor o = o_in->defined() ? *o_in : at::empty(q->sizes(), q->options());
+    const Tensor lse = lse_in->defined() ? *lse_in : at::empty(q->sizes().slice(0, 3), q->options().dtype(at::kFloat));
+    if (o.sizes() != q->sizes() || !view4(o, &to)) {
+        if (!PyErr_Occurred()) bad("o must be shaped like q");
+        return nullptr;
+    }
+    if (lse.scalar_type() != at::kFloat || !lse.is_contiguous() || lse.sizes() != q->sizes().slice(0, 3)) { bad("lse must be a contiguous float32 tensor shaped like q without its last axis"); return nullptr; }
+    void* s = stream_of(g);
+    const obc_status st = unlocked([&] { return obc_paged_attention(&g.c, &p, tq, to, ptr<float>(lse), ws.data_ptr(), ws.nbytes(), s); });
+    return st == OBC_OK ? tuple_of({o, lse}) : status(st);
+    END_HANDLE_TH_ERRORS
+}
+
 #define OBC_METHOD(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {OBC_METHOD("score", n_score), OBC_METHOD("select", n_select), OBC_METHOD("compact", n_compact),
-                         OBC_METHOD("evict", n_evict), OBC_METHOD("decode_step", n_decode), {nullptr, nullptr, 0, nullptr}};
+                         OBC_METHOD("evict", n_evict), OBC_METHOD("decode_step", n_decode),
+                         OBC_METHOD("paged_write", n_paged_write), OBC_METHOD("paged_read", n_paged_read),
+                         OBC_METHOD("paged_attention", n_paged_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods};
 
 }  // namespace

@@ -15,7 +15,7 @@
 //                  the evictable slots
 //   decode_final   per (b, g): pick the slot to free, update pos / state
 // Few units take one kernel for all of it instead (decode_fused.cuh).
-#include "obc_common.cuh"
+#include "warp_mma.cuh"
 
 #include <cooperative_groups.h>
 namespace cg = cooperative_groups;
@@ -115,19 +115,6 @@ __device__ __forceinline__ int staged_piece(int row, int piece) {
 // was what limited the blocks in flight.  One m16n8k16 MMA per 16 slots and 16 channels replaces 128
 // multiply-adds per lane; the operands come out of the staged rows with ldmatrix (the 16-byte pieces of
 // the swizzled rows are exactly its 8x8 tiles).
-__device__ __forceinline__ void ldsm_x4(uint32_t (&r)[4], const void* p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"((uint32_t)__cvta_generic_to_shared(p)));
-}
-__device__ __forceinline__ void ldsm_x4_trans(uint32_t (&r)[4], const void* p) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"((uint32_t)__cvta_generic_to_shared(p)));
-}
-// d += a (16x16, row-major) * b (16x8, column-major), bf16 operands, fp32 accumulators
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 // address of the 8x8 tile that lane `lane` names for an x4 load covering 16 staged rows from `row0` and the two
 // 16-byte pieces `piece0`, `piece0 + 1`.  rows_major: tiles ordered (rows 0-7, p0), (rows 8-15, p0), (rows 0-7, p1),
 // (rows 8-15, p1), the A operand of slots x channels; otherwise (rows 0-7, p0), (rows 0-7, p1), (rows 8-15, p0), ...
@@ -138,14 +125,6 @@ __device__ __forceinline__ const uint4* tile_addr(const uint4* sRows, int row0, 
     const int piece = piece0 + (rows_major ? (mi >> 1) : (mi & 1));
     return sRows + staged_piece<N>(row, piece);
 }
-// x = hi + lo with both halves bf16: two MMAs then carry an fp32 operand to about 16 bits
-__device__ __forceinline__ void split_bf16x2(float x0, float x1, uint32_t& hi, uint32_t& lo) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1);
-    const __nv_bfloat162 l = __floats2bfloat162_rn(x0 - __low2float(h), x1 - __high2float(h));
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
-}
-
 // Eq. 4-6 (or the attention-only score) of one slot for the newest query of G heads: log2-scaled logits z2, log2-sum-exp, |o|^2
 // and v . o per head, |v|^2
 template <int G>

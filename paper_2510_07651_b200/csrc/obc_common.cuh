@@ -136,11 +136,46 @@ obc_status launch_score_tc(const ScoreShape& s, TensorView q, TensorView k, Tens
                            float* scores, void* ws, cudaStream_t stream, const GivenAttention* given = nullptr,
                            SimtPlan* attention_only = nullptr);   // non-null: stop after pass 1 + combine, return the plan
 
+// ---- paged caches -----------------------------------------------------------------------------------
+struct PagesView {                       // a paged cache as the kernels see it
+    int B, Hkv, n_pages, P, max_pages, max_len;
+    int dtype;
+    TensorView k, v;                     // sb: from page to page
+    uint8_t *ks, *vs;
+    long long ss_p, ss_h;
+    const int32_t* table; long long tb, th;
+    const int32_t* lens; long long lb, lh;
+    __device__ __forceinline__ int len(int b, int h) const { return min(max(lens[b * lb + h * lh], 0), max_len); }
+    // page that holds token t of list (b, h); negative if the table names none
+    __device__ __forceinline__ int page_of(int b, int h, int t) const {
+        const int page = table[b * tb + h * th + t / P];
+        return (unsigned)page < (unsigned)n_pages ? page : -1;
+    }
+};
+struct PagedWrite {
+    int rows, src_tokens, src_dtype;
+    const int32_t* new_lens; long long nb, nh;
+    const int32_t* idx;
+};
+obc_status launch_paged_write(const PagesView& c, const PagedWrite& w, TensorView k, TensorView v, cudaStream_t stream);
+obc_status launch_paged_read(const PagesView& c, int n_tokens, int out_dtype, TensorView k, TensorView v, bool zero_rows, cudaStream_t stream);
+struct AttnShape {
+    int Hq, G, T;
+    const int32_t* q_lens;
+    float scale;
+    int causal;
+};
+size_t paged_attention_bytes(const PagesView& c, const AttnShape& s);
+obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, TensorView q, TensorView o, float* lse, void* ws, cudaStream_t stream);
+
 // ---- tensor maps ----------------------------------------------------------------------------------
 // bf16 tensor map of rank 2 to 4 with 128-byte swizzle, innermost dimension = head_dim (128), box
 // {64, box_rows, 1, 1}; strides in bytes for dimensions 1..rank-1.  Maps are cached per host thread.
 bool make_map(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
               uint32_t box_rows);
+// the pages of a paged cache (bf16 or e4m3): dimensions channel, token of the page, head, page; box of 128 bytes of `box` tokens,
+// 128-byte swizzle.  A negative page number reads as zeros.
+bool make_page_map(CUtensorMap* map, const PagesView& c, const TensorView& t, int box);
 
 // ---- programmatic dependent launch ------------------------------------------------------------
 // Every kernel of the library is launched with programmatic stream serialization: its CTAs may

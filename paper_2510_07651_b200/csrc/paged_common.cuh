@@ -1,0 +1,142 @@
+// What the kernels of obc_paged_attention share: how the work is cut into pieces, and where partial results go.
+//
+// An item is a tile of `ROWS` query rows of one KV list (row r = i G + g is query i of the group's head g, so that a tile's rows are near
+// one another in position and stop at the same tokens).  An item costs as many token tiles of 128 as its last row sees.  All items, in
+// order, are cut into a run of equal cost per CTA, so that ragged batches, lists per head and causal chunks load every CTA alike
+// whatever the lengths, which only the device knows.  A CTA's run is a sequence of segments, each a range of tiles of one item.  An
+// item that lies within one run is finished there; the others leave partial results (maximum, sum, unnormalised output) that the
+// merge kernel joins in the order of the tiles.  A run has at most two such segments, its first and its last.
+#pragma once
+#include "obc_common.cuh"
+
+namespace obc {
+namespace {
+
+constexpr int kTokTile = 128;
+
+struct AttnParams {
+    PagesView c;
+    int G, T, causal;
+    const int32_t* q_lens;
+    float sl2;                               // scale * log2(e)
+    TensorView q, o;
+    float* lse;                              // or nullptr
+    int nrt, items;                          // row tiles per list, items in all
+    int box, one_head;                       // tokens per bulk copy; pages of one head
+    unsigned int* status;                    // workspace header: source line of the wait that gave up
+    int4* info;                              // per item: first and last CTA and the first one's slot; x < 0: finished by one CTA
+    float *part_m, *part_l, *part_o;         // [2 gridDim][ROWS] (x d): slots of a CTA's first and last segment
+};
+
+struct Item { int b, h, len, ql, r0, rows, tiles; };      // rows: rows of this tile; tiles: 0 if it has none
+
+template <int ROWS>
+__device__ __forceinline__ Item item_of(const AttnParams& p, int it) {
+    Item m;
+    const int unit = it / p.nrt;
+    m.b = unit / p.c.Hkv; m.h = unit - m.b * p.c.Hkv;
+    m.len = p.c.len(m.b, m.h);
+    m.ql = p.q_lens ? min(max(p.q_lens[m.b], 0), p.T) : p.T;
+    m.r0 = (it - unit * p.nrt) * ROWS;
+    m.rows = min(p.G * m.ql - m.r0, ROWS);
+    m.tiles = 0;
+    if (m.rows > 0) {                        // (one tile at least: rows that see nothing have results, too)
+        const int seen = p.causal ? min(max(m.len - m.ql + (m.r0 + m.rows - 1) / p.G + 1, 0), m.len) : m.len;
+        m.tiles = max((seen + kTokTile - 1) / kTokTile, 1);
+    }
+    return m;
+}
+// tokens that row r of the item's tile sees: p < the result (r beyond the tile's rows: none)
+__device__ __forceinline__ int seen_by(const AttnParams& p, const Item& m, int r) {
+    if (r >= m.rows) return 0;
+    return p.causal ? min(max(m.len - m.ql + (m.r0 + r) / p.G + 1, 0), m.len) : m.len;
+}
+
+struct Run { long long begin, end, total, ctas; int item, off; };
+struct RunScratch { long long warp_sum[32]; Run run; };
+
+// This CTA's run; all threads of the block take part.
+template <int ROWS>
+__device__ __forceinline__ Run find_run(const AttnParams& p, RunScratch* s) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nwarps = blockDim.x >> 5;
+    const int per = (p.items + blockDim.x - 1) / blockDim.x, i0 = tid * per, i1 = min(i0 + per, p.items);
+    long long mine = 0;
+    for (int i = i0; i < i1; ++i) mine += item_of<ROWS>(p, i).tiles;
+    long long scan = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
+    }
+    if (lane == 31) s->warp_sum[warp] = scan;
+    __syncthreads();
+    long long before = scan - mine, total = 0;
+    for (int w = 0; w < nwarps; ++w) {
+        if (w < warp) before += s->warp_sum[w];
+        total += s->warp_sum[w];
+    }
+    // (no empty runs between two others: the merge goes by CTA numbers)
+    const long long ctas = min((long long)gridDim.x, total);
+    const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : total, end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
+    if (tid == 0) { s->run.begin = begin; s->run.end = end; s->run.total = total; s->run.ctas = ctas; s->run.item = 0; s->run.off = 0; }
+    __syncthreads();
+    if (begin >= before && begin < before + mine) {
+        long long at = before;
+        for (int i = i0; i < i1; ++i) {
+            const int n = item_of<ROWS>(p, i).tiles;
+            if (begin < at + n) { s->run.item = i; s->run.off = (int)(begin - at); break; }
+            at += n;
+        }
+    }
+    __syncthreads();
+    return s->run;
+}
+
+// Walks the segments of a run; every role of a CTA has its own copy.
+template <int ROWS>
+struct Segments {
+    const AttnParams& p;
+    long long at, end;
+    int next_item, off;
+    Item m;                                  // the segment: tiles [ta, tb) of item `item`
+    int item, ta, tb;
+    bool first;
+    __device__ __forceinline__ Segments(const AttnParams& p_, const Run& r) : p(p_), at(r.begin), end(r.end), next_item(r.item), off(r.off), first(true) { item = -1; }
+    __device__ __forceinline__ bool next() {
+        if (item >= 0) first = false;
+        if (at >= end) return false;
+        for (;; ++next_item) {
+            m = item_of<ROWS>(p, next_item);
+            if (m.tiles > 0) break;
+        }
+        item = next_item; ta = off;
+        tb = (int)min((long long)m.tiles, off + (end - at));
+        at += tb - ta;
+        ++next_item; off = 0;
+        return true;
+    }
+    __device__ __forceinline__ bool whole() const { return ta == 0 && tb == m.tiles; }
+    __device__ __forceinline__ size_t slot() const { return 2 * (size_t)blockIdx.x + (first ? 0 : 1); }
+};
+
+// the CTA that an item begins in says how it is shared out
+template <int ROWS>
+__device__ __forceinline__ void note_item(const AttnParams& p, const Run& r, const Segments<ROWS>& s) {
+    if (s.ta != 0) return;
+    int4 v = make_int4(-1, -1, 0, 0);
+    if (!s.whole()) {
+        const long long last = s.at - (s.tb - s.ta) + s.m.tiles - 1;          // the item's last tile
+        v = make_int4((int)blockIdx.x, (int)(((last + 1) * r.ctas + r.total - 1) / r.total) - 1, s.first ? 0 : 1, 0);
+    }
+    p.info[s.item] = v;
+}
+
+// where the row (i G + g) of an item's list stands in q, o and lse
+__device__ __forceinline__ void row_place(const AttnParams& p, const Item& m, int r, int& head, int& i) {
+    const int row = m.r0 + r;
+    i = row / p.G;
+    head = m.h * p.G + (row - i * p.G);
+}
+
+}  // namespace
+}  // namespace obc
