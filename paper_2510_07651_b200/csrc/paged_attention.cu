@@ -3,20 +3,17 @@
 //
 //   few_rows_kernel      up to 32 rows per KV list (single tokens of a GQA group): bound by the K/V bytes.  Pages arrive as bulk copies
 //                        (TMA) in a ring; eight warps take 16 tokens of every 128-token tile each and run warp-level MMAs.
+//   chunk_kernel         more rows: tcgen05 MMAs (paged_chunk.cuh)
 //   paged_f32_kernel     fp32 caches on CUDA cores
 //   paged_merge_kernel   joins the partial results of items that several CTAs shared
 // How the work is shared out: paged_common.cuh.
-#include "paged_common.cuh"
-#include "tc_ptx.cuh"
+#include "paged_chunk.cuh"
 #include "warp_mma.cuh"
 
 #include <math.h>
 
 namespace obc {
 namespace {
-
-// natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)
-__device__ __forceinline__ float lse_of(float ref, float total) { return (ref + log2f(total)) * 0.6931471805599453f; }
 
 // ---- merge ------------------------------------------------------------------------------------------
 // One warp per row of an item that was shared: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the CTAs' slots, in
@@ -84,11 +81,7 @@ template <bool E4M3> struct FewLayout {
     static constexpr uint32_t kSmem = kEnd + 1024;                                         // + alignment slack
 };
 
-// bytes b0..b3 of x (e4m3 codes) as bf16 pairs, each value times 2^-120: (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3)
-__device__ __forceinline__ void expand(uint32_t x, uint32_t& lo, uint32_t& hi) {
-    lo = (x << 4) & 0xf0f0f0f0u;
-    hi = (x & 0x80808080u) | ((x >> 4) & 0x07070707u);
-}
+// (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3), of four codes as bf16 pairs, each value times 2^-120
 __device__ __forceinline__ void expand_adjacent(uint32_t x, uint32_t& p01, uint32_t& p23) {
     uint32_t lo, hi;
     expand(x, lo, hi);
@@ -651,7 +644,7 @@ struct AttnPlan { int rows, grid, nrt, items; size_t off_info, off_m, off_l, off
 AttnPlan make_plan(const PagesView& c, const AttnShape& s) {
     AttnPlan p{};
     const long long rows = (long long)s.G * s.T;
-    p.rows = c.dtype == OBC_F32 ? kF32Rows : rows <= 16 ? 16 : 32;
+    p.rows = c.dtype == OBC_F32 ? kF32Rows : rows <= 16 ? 16 : rows <= 32 ? 32 : kChunkRows;
     p.grid = sm_count() * (c.dtype == OBC_F32 ? 2 : 1);
     p.nrt = (int)((rows + p.rows - 1) / p.rows);
     p.items = c.B * c.Hkv * p.nrt;
@@ -696,7 +689,19 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
             ProfScope prof("paged_attention_few", stream);
             return launch_pdl(kernel, dim3(plan.grid), dim3(kFewThreads), smem, stream, 1, mk, mv, p);
         };
-        if (c.dtype == OBC_E4M3)
+        auto chunk = [&](auto kernel, size_t smem, int threads, int regs) {
+            cudaFuncAttributes fa{};
+            cudaError_t a = cudaFuncGetAttributes(&fa, kernel);
+            if (a != cudaSuccess) return a;
+            if (fa.numRegs < regs) return cudaErrorInvalidKernelImage;      // its warps would wait for registers that the launch does not bring
+            if ((a = allow_smem(kernel, smem)) != cudaSuccess) return a;
+            ProfScope prof("paged_attention_chunk", stream);
+            return launch_pdl(kernel, dim3(plan.grid), dim3(threads), smem, stream, 1, mk, mv, p);
+        };
+        if (plan.rows == kChunkRows)
+            e = c.dtype == OBC_E4M3 ? chunk(chunk_kernel<true>, ChunkLayout<true>::kSmem, ChunkLayout<true>::kThreads, 128)
+                                    : chunk(chunk_kernel<false>, ChunkLayout<false>::kSmem, ChunkLayout<false>::kThreads, 168);
+        else if (c.dtype == OBC_E4M3)
             e = plan.rows == 16 ? few(few_rows_kernel<1, true>, FewLayout<true>::kSmem) : few(few_rows_kernel<2, true>, FewLayout<true>::kSmem);
         else
             e = plan.rows == 16 ? few(few_rows_kernel<1, false>, FewLayout<false>::kSmem) : few(few_rows_kernel<2, false>, FewLayout<false>::kSmem);
@@ -708,7 +713,8 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
     };
     OBC_CUDA_TRY(c.dtype == OBC_F32 ? merge(paged_merge_kernel<float, 16>)
                  : plan.rows == 16  ? merge(paged_merge_kernel<__nv_bfloat16, 16>)
-                                    : merge(paged_merge_kernel<__nv_bfloat16, 32>));
+                 : plan.rows == 32  ? merge(paged_merge_kernel<__nv_bfloat16, 32>)
+                                    : merge(paged_merge_kernel<__nv_bfloat16, kChunkRows>));
     return OBC_OK;
 }
 

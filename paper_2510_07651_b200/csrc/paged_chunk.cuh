@@ -1,0 +1,510 @@
+// Attention of many rows per KV list (chunks of a prompt) over a paged cache: tcgen05 MMAs with TMEM accumulators.
+//
+// A CTA works on 256 query rows of a list, 128 per softmax warpgroup, one row per thread.  For tile i of 128 tokens and warpgroup w:
+//     S_w  = Q_w K_i^T                       accumulator in TMEM
+//     P_w  = 2^(S_w scale log2 e - m_w)      registers -> bf16 -> TMEM, over S_w's first 64 columns
+//     O_w += P_w V_i                         A operand from TMEM, V as MN-major B
+// While one warpgroup is at its exponentials the MMAs of the other run; a K or V tile is fetched once for both.  m_w only moves when a
+// tile's maximum exceeds it by more than 2^8, so that O_w is rescaled (in TMEM, by the thread that owns the row) a few times per
+// list.  MMAs issued by one thread execute in order: S_w(i+1) cannot overwrite P_w(i) before P_w V(i) has read it, and the
+// commit behind S_w(i+1) covers P_w V(i).
+//
+//   warp 0       producer: pages -> ring of 32 KB operands (K and V tiles in turn); 8-bit pages -> ring of raw tiles and their scales
+//   warp 1       MMA issuer
+//   warps 2-3    Q of the next segment; warp 2: V tiles at a list's end: rows behind it become zeros, rows that are not finite and that not
+//                every query sees become zeros, too, and are named to the softmax warps, which add them by hand where they are seen
+//   warps 4-11   softmax, two warpgroups
+//   warps 12-15  (8-bit pages) codes -> bf16 tiles, the scale multiplied in exactly; and what warp 2 does for V tiles
+// TMEM columns: S_0 [0,128)  S_1 [128,256)  O_0 [256,384)  O_1 [384,512)
+#pragma once
+#include "paged_common.cuh"
+#include "tc_ptx.cuh"
+
+namespace obc {
+namespace {
+
+constexpr int kChunkRows = 256;
+
+template <bool E4M3> struct ChunkLayout {
+    static constexpr int kThreads = E4M3 ? 512 : 384;
+    static constexpr int kSlots = E4M3 ? 4 : 5;                                        // bf16 operands of 32 KB
+    static constexpr int kRaw = E4M3 ? 2 : 0;                                          // raw operands of 16 KB
+    static constexpr uint32_t kQ = 0, kRing = 2 * kOperandBytes, kRawAt = kRing + kSlots * kOperandBytes;
+    static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
+    static constexpr uint32_t kBad = kScales + kRaw * 128u;                            // [slot][4] words: tokens to be added by hand
+    static constexpr uint32_t kBars = kBad + kSlots * 16u;
+    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, QEMPTY, SFULL, PFULL = SFULL + 2, ODONE = PFULL + 2, RAWFULL = ODONE + 2,
+           RAWEMPTY = RAWFULL + 2, NBARS = RAWEMPTY + 2 };
+    static constexpr uint32_t kTmem = kBars + NBARS * 8u;
+    static constexpr uint32_t kSmem = kTmem + 16 + 1024;
+    // registers: softmax warpgroups against the others, out of what the launch gives all threads
+    static constexpr int kSoftRegs = E4M3 ? 184 : 208, kOtherRegs = E4M3 ? 72 : 88;
+    static_assert(256 * kSoftRegs + (kThreads - 256) * kOtherRegs <= kThreads * (E4M3 ? 128 : 168), "registers");
+};
+
+// a segment as the roles of the CTA see it
+struct ChunkSeg {
+    int n, cnt0, cnt1;                       // tiles; of warpgroup 0 and 1 (from the segment's first tile on)
+    int first_masked;                        // tokens from here on are not seen by every row of the item
+    __device__ __forceinline__ int cnt(int w) const { return w ? cnt1 : cnt0; }
+};
+__device__ __forceinline__ ChunkSeg chunk_seg(const AttnParams& p, const Segments<kChunkRows>& s) {
+    ChunkSeg c;
+    c.n = s.tb - s.ta;
+    const int t0 = max((seen_by(p, s.m, min(s.m.rows, 128) - 1) + kTokTile - 1) / kTokTile, 1);
+    const int t1 = s.m.rows > 128 ? (seen_by(p, s.m, s.m.rows - 1) + kTokTile - 1) / kTokTile : 0;
+    c.cnt0 = min(max(min(t0, s.tb) - s.ta, 0), c.n);
+    c.cnt1 = min(max(min(t1, s.tb) - s.ta, 0), c.n);
+    c.first_masked = seen_by(p, s.m, 0);
+    return c;
+}
+
+__device__ __forceinline__ void tc_ld1(uint32_t taddr, uint32_t& r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0x7f80u) == 0x7f80u || (bf16x2 & 0x7f800000u) == 0x7f800000u; }
+template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// four bytes (e4m3 codes) -> two bf16 pairs, times m1 * m2 (powers of two that leave the product exact)
+__device__ __forceinline__ void codes_to_bf16(uint32_t x, __nv_bfloat162 m1, __nv_bfloat162 m2, bool two, uint32_t& p01, uint32_t& p23) {
+    uint32_t lo, hi;
+    expand(x, lo, hi);
+    const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+    __nv_bfloat162 u = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), m1), v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), m1);
+    if (two) { u = __hmul2(u, m2); v = __hmul2(v, m2); }
+    p01 = *reinterpret_cast<const uint32_t*>(&u); p23 = *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <bool E4M3>
+__global__ void __launch_bounds__(ChunkLayout<E4M3>::kThreads, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnParams p) {
+    using L = ChunkLayout<E4M3>;
+    constexpr int NS = L::kSlots;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem);
+    __shared__ RunScratch scratch;
+    auto bar = [&](int i) { return sbase + L::kBars + 8u * (uint32_t)i; };
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + L::kTmem);
+    uint32_t* bad_words = reinterpret_cast<uint32_t*>(smem + L::kBad);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
+        for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 1); mbar_init(bar(L::EDGE + i), 1); }
+        mbar_init(bar(L::QFULL), 64); mbar_init(bar(L::QEMPTY), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
+            mbar_init(bar(L::RAWFULL + i), 33); mbar_init(bar(L::RAWEMPTY + i), 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(sbase + L::kTmem), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0u;        // no wait of this call can have given up yet (each lasts seconds)
+    const Run run = find_run<kChunkRows>(p, &scratch);
+    int fail_site = 0;
+    auto wait = [&](int b, uint32_t parity, int line) -> bool {
+        if (mbar_wait(bar(b), parity & 1u)) return true;
+        fail_site = line;
+        return false;
+    };
+    // V tiles that reach behind what every row sees pass through warp 2 before anyone else may read them (16-bit pages): their copies complete
+    // on the slot's EDGE barrier, whose parity warp 2 keeps (a bit per slot), and warp 2 arrives on FULL in their stead.
+    auto is_edge = [&](const ChunkSeg& c, int t0) { return t0 + kTokTile > c.first_masked; };
+
+    if (warp < 4) {
+        fewer_registers<L::kOtherRegs>();
+        if (warp == 0) {
+            // ===================================== producer =====================================
+            Segments<kChunkRows> seg(p, run);
+            bool more = seg.next();
+            int tile = seg.ta;
+            auto page_at = [&]() -> int {                           // the lane's box of the current tile
+                const int t = tile * kTokTile + lane * p.box;
+                return lane < kTokTile / p.box && t < seg.m.len ? p.c.page_of(seg.m.b, seg.m.h, t) : -1;
+            };
+            int page = more ? page_at() : -1;
+            uint32_t n = 0;                                         // operands issued
+            while (more && !fail_site) {
+                const int pg = page, h = seg.m.h, t0 = tile * kTokTile;
+                const bool edge = t0 + kTokTile > seen_by(p, seg.m, 0);
+                if (++tile == seg.tb) { more = seg.next(); tile = seg.ta; }
+                if (more) page = page_at();                         // the next tile's page numbers travel meanwhile
+                const int boxes = kTokTile / p.box, slot = (t0 + lane * p.box) % p.c.P, hh = p.one_head ? 0 : h;
+                for (int op = 0; op < 2; ++op, ++n) {
+                    const CUtensorMap* map = op ? &map_v : &map_k;
+                    if (E4M3) {
+                        const uint32_t st = n & 1, full = bar(L::RAWFULL + st);
+                        if (!wait(L::RAWEMPTY + st, (n >> 1) ^ 1u, __LINE__)) break;
+                        if (lane == 0) mbar_expect_tx(full, 16384);
+                        __syncwarp();
+                        if (lane < boxes) tma_load_4d(sbase + L::kRawAt + st * 16384u + lane * p.box * 128, map, full, 0, slot, hh, pg);
+                        const int t8 = (lane & 15) * 8, ps = __shfl_sync(0xffffffffu, pg, t8 / p.box);
+                        if (lane < 16) {
+                            const uint8_t* src = (op ? p.c.vs : p.c.ks) + (ps < 0 ? 0ll : ps * p.c.ss_p + h * p.c.ss_h + (t0 + t8) % p.c.P);
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(sbase + L::kScales + st * 128u + t8), "l"(src), "r"(ps < 0 ? 0 : 8) : "memory");
+                        }
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
+                    } else {
+                        const uint32_t st = n % NS, full = bar((op && edge ? L::EDGE : L::FULL) + st);
+                        if (!wait(L::EMPTY + st, (n / NS) ^ 1u, __LINE__)) break;
+                        if (lane == 0) mbar_expect_tx(full, kOperandBytes);
+                        __syncwarp();
+                        if (lane < boxes) {
+                            const uint32_t d = sbase + L::kRing + st * kOperandBytes + lane * p.box * 128;
+                            tma_load_4d(d, map, full, 0, slot, hh, pg);
+                            tma_load_4d(d + kHalfBytes, map, full, 64, slot, hh, pg);
+                        }
+                    }
+                }
+            }
+            // no copy may be under way when the CTA leaves
+            const uint32_t ring = E4M3 ? 2u : (uint32_t)NS;
+            for (uint32_t back = 0; back < ring && back < n; ++back) {
+                const uint32_t k = n - 1 - back;
+                (void)mbar_wait(bar((E4M3 ? (int)L::RAWFULL : (int)L::FULL) + k % ring), (k / ring) & 1u);
+            }
+        } else if (warp == 1) {
+            // ===================================== MMA issuer =======================================
+            if (lane == 0) {
+                const uint32_t idesc_s = idesc_bf16(kTokTile);
+                const uint32_t idesc_pv = idesc_bf16(kD) | (1u << 16);           // B operand (V) is MN-major
+                Segments<kChunkRows> seg(p, run);
+                uint32_t base = 0, np[2] = {0, 0}, q_n = 0;                      // tiles before this segment; P tiles taken; segments
+                while (!fail_site && seg.next()) {
+                    const ChunkSeg c = chunk_seg(p, seg);
+                    auto slot_of = [&](int i, int op) { return (2 * (base + i) + op) % NS; };
+                    auto full = [&](int i, int op, int line) { return wait(L::FULL + slot_of(i, op), (2 * (base + i) + op) / NS, line); };
+                    auto issue_s = [&](int w, int i) {
+                        const uint32_t ak = desc_lo_k(sbase + L::kRing + slot_of(i, 0) * kOperandBytes), aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes);
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks)
+                            tc_mma(tmem + w * 128u, desc_make(aq + desc_kstep(ks, kHalfBytes)), desc_make(ak + desc_kstep(ks, kHalfBytes)), idesc_s, ks > 0);
+                        tc_commit(bar(L::SFULL + w));
+                    };
+                    if (!wait(L::QFULL, q_n, __LINE__) || !full(0, 0, __LINE__)) break;
+                    ++q_n;
+                    tc_fence_after();
+                    if (c.cnt0 > 0) issue_s(0, 0);
+                    if (c.cnt1 > 0) issue_s(1, 0);
+                    tc_commit(bar(L::EMPTY + slot_of(0, 0)));
+                    if (c.n == 1) tc_commit(bar(L::QEMPTY));
+                    for (int i = 0; i < c.n && !fail_site; ++i) {
+                        const int vs = slot_of(i, 1);
+                        if (!full(i, 1, __LINE__)) break;
+                        const int last = i < c.cnt1 ? 1 : 0;                 // the last warpgroup that reads V_i
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            if (i < c.cnt(w)) {
+                                if (!wait(L::PFULL + w, np[w], __LINE__)) break;
+                                ++np[w];
+                                tc_fence_after();
+                                const uint32_t av = desc_lo_mn(sbase + L::kRing + vs * kOperandBytes);
+#pragma unroll
+                                for (int ks = 0; ks < 8; ++ks)           // 128 tokens = 8 steps of K = 16 (2048 bytes of V each)
+                                    tc_mma_ts(tmem + 256u + w * 128u, tmem + w * 128u + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
+                                if (w == last) tc_commit(bar(L::EMPTY + vs));
+                                if (i == c.cnt(w) - 1) tc_commit(bar(L::ODONE + w));
+                            }
+                            if (i + 1 < c.cnt(w)) {
+                                if (!full(i + 1, 0, __LINE__)) break;
+                                issue_s(w, i + 1);
+                            }
+                        }
+                        if (fail_site) break;
+                        if (i + 1 < c.n) {
+                            tc_commit(bar(L::EMPTY + slot_of(i + 1, 0)));
+                            if (i + 2 == c.n) tc_commit(bar(L::QEMPTY));
+                        }
+                    }
+                    base += c.n;
+                }
+            }
+        } else {
+            // ======================= Q tiles; V tiles at the end of what is seen =======================
+            const int t64 = threadIdx.x - 64;
+            Segments<kChunkRows> seg(p, run);
+            uint32_t base = 0, q_n = 0, edges = 0;
+            while (!fail_site && seg.next()) {
+                const Item& m = seg.m;
+                const ChunkSeg c = chunk_seg(p, seg);
+                if (!wait(L::QEMPTY, q_n ^ 1u, __LINE__)) break;
+                ++q_n;
+                const int rows = m.rows > 128 ? 256 : 128, piece = t64 & 15;
+#pragma unroll 4
+                for (int r = t64 >> 4; r < rows; r += 4) {          // sixteen lanes per row; rows that are not there become zeros
+                    int head = 0, i = 0;
+                    if (r < m.rows) row_place(p, m, r, head, i);
+                    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.ptr) + m.b * p.q.sb + head * p.q.sh + i * p.q.st + piece * 8;
+                    const int rr = r & 127;
+                    const uint32_t dst = sbase + L::kQ + (r >> 7) * kOperandBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(r < m.rows ? 16 : 0) : "memory");
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_async_smem();
+                mbar_arrive(bar(L::QFULL));
+                if (!E4M3 && warp == 2) {
+                    for (int i = 0; i < c.n; ++i) {
+                        const int t0 = (seg.ta + i) * kTokTile;
+                        if (!is_edge(c, t0)) continue;
+                        const uint32_t op = 2 * (base + i) + 1;
+                        const int vs = op % NS;
+                        if (!wait(L::EDGE + vs, edges >> vs, __LINE__)) break;
+                        edges ^= 1u << vs;
+                        uint8_t* tile = smem + L::kRing + vs * kOperandBytes;
+#pragma unroll 1
+                        for (int j = 0; j < 4; ++j) {
+                            const int row = j * 32 + lane, t = t0 + row;
+                            bool odd = false;
+                            if (t >= c.first_masked && t < m.len) {
+#pragma unroll
+                                for (int ch = 0; ch < 16; ++ch) {
+                                    const uint4 u = *reinterpret_cast<const uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+                                    odd |= not_finite(u.x) || not_finite(u.y) || not_finite(u.z) || not_finite(u.w);
+                                }
+                            }
+                            if (odd || t >= m.len) {
+#pragma unroll
+                                for (int ch = 0; ch < 16; ++ch)
+                                    *reinterpret_cast<uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            const uint32_t word = __ballot_sync(0xffffffffu, odd);
+                            if (lane == 0) bad_words[vs * 4 + j] = word;
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(L::FULL + vs));
+                    }
+                }
+                base += c.n;
+            }
+        }
+    } else if (warp < 12) {
+        // ======================================= softmax ========================================
+        more_registers<L::kSoftRegs>();
+        const int w = (warp - 4) >> 2, lane_grp = warp & 3, row = lane_grp * 32 + lane, r = w * 128 + row;
+        const uint32_t lane_addr = (uint32_t)(lane_grp * 32) << 16;
+        const uint32_t tS = tmem + lane_addr + w * 128u, tO = tmem + lane_addr + 256u + w * 128u;
+        const float2 sl2v = make_float2(p.sl2, p.sl2);
+        Segments<kChunkRows> seg(p, run);
+        uint32_t base = 0, ns = 0, no = 0;
+        while (!fail_site && seg.next()) {
+            const Item& m = seg.m;
+            const ChunkSeg c = chunk_seg(p, seg);
+            const int cnt = c.cnt(w), seen = seen_by(p, m, r);
+            float m_used = -INFINITY, l = 0.f;
+            if (cnt > 0) {                                          // O starts at 0 (all of its MMAs accumulate)
+                uint32_t z[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) z[j] = 0u;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tc_st32(tO + q * 32, z);
+                tc_wait_st();                                       // (ordered before the MMAs by the first P's barrier)
+            }
+            for (int i = 0; i < c.n; ++i) {
+                const int t0 = (seg.ta + i) * kTokTile, vs = (2 * (base + i) + 1) % NS;
+                const bool edge = is_edge(c, t0);
+                if (i < cnt) {
+                    if (!wait(L::SFULL + w, ns, __LINE__)) break;
+                    ++ns;
+                    tc_fence_after();
+                    uint32_t s[128];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tc_ld32(tS + q * 32, s + q * 32);
+                    tc_wait_ld32(s);
+#pragma unroll
+                    for (int q = 1; q < 4; ++q) tc_wait_ld32(s + q * 32);
+                    const int nvis = seen - t0;                     // columns j < nvis are seen
+                    if (edge && __any_sync(0xffffffffu, nvis < kTokTile)) {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) if (j >= nvis) s[j] = 0xff800000u;
+                    }
+                    float t4[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        t4[q] = fmaxf(__uint_as_float(s[q]), __uint_as_float(s[q + 4]));
+#pragma unroll
+                        for (int j = 8; j < 128; j += 8) t4[q] = fmax3(t4[q], __uint_as_float(s[j + q]), __uint_as_float(s[j + q + 4]));
+                    }
+                    const float mt = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.sl2;
+                    const bool need = mt > m_used + 8.f;            // also true for the first tile that is seen
+                    if (__any_sync(0xffffffffu, need)) {
+                        const float factor = need ? fast_exp2(m_used - mt) : 1.f;
+                        if (__any_sync(0xffffffffu, need && m_used != -INFINITY)) {
+                            // P V of this warpgroup's previous tile is complete (the commit that signalled S covers it)
+#pragma unroll 1
+                            for (int q = 0; q < 8; ++q) {
+                                uint32_t ov[16];
+                                tc_ld16(tO + q * 16, ov);
+                                asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(ov[0]), "+r"(ov[1]), "+r"(ov[2]), "+r"(ov[3]), "+r"(ov[4]), "+r"(ov[5]), "+r"(ov[6]), "+r"(ov[7]),
+                                             "+r"(ov[8]), "+r"(ov[9]), "+r"(ov[10]), "+r"(ov[11]), "+r"(ov[12]), "+r"(ov[13]), "+r"(ov[14]), "+r"(ov[15]) :: "memory");
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * factor);
+                                tc_st16(tO + q * 16, ov);
+                            }
+                        }
+                        l *= factor;
+                        if (need) m_used = mt;
+                    }
+                    const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+                    const float2 negm = make_float2(-m_eff, -m_eff);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            float2 x = make_float2(__uint_as_float(s[q * 32 + j]), __uint_as_float(s[q * 32 + j + 1]));
+                            x = __ffma2_rn(x, sl2v, negm);
+                            const float2 ex = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+                            sum[(j >> 1) & 1] = __fadd2_rn(sum[(j >> 1) & 1], ex);
+                            pk[j >> 1] = pack_bf16x2(ex.x, ex.y);
+                        }
+                        tc_st16(tS + q * 16, pk);
+                    }
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+                    tc_wait_st();
+                    if (edge) {                                     // rows of V that are added by hand
+                        if (!wait(L::FULL + vs, (2 * (base + i) + 1) / NS, __LINE__)) break;
+#pragma unroll 1
+                        for (int b = 0; b < 4; ++b) {
+                            uint32_t word = bad_words[vs * 4 + b];
+                            while (word) {
+                                const int j = b * 32 + __ffs(word) - 1;
+                                word &= word - 1;
+                                uint32_t two;
+                                tc_ld1(tS + (j >> 1), two);
+                                const float wt = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+                                const int t = t0 + j, page = E4M3 ? -1 : p.c.page_of(m.b, m.h, t);
+#pragma unroll 1
+                                for (int q = 0; q < 8; ++q) {
+                                    uint32_t ov[16];
+                                    tc_ld16(tO + q * 16, ov);
+                                    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(ov[0]), "+r"(ov[1]), "+r"(ov[2]), "+r"(ov[3]), "+r"(ov[4]), "+r"(ov[5]), "+r"(ov[6]), "+r"(ov[7]),
+                                                 "+r"(ov[8]), "+r"(ov[9]), "+r"(ov[10]), "+r"(ov[11]), "+r"(ov[12]), "+r"(ov[13]), "+r"(ov[14]), "+r"(ov[15]) :: "memory");
+#pragma unroll
+                                    for (int x = 0; x < 16; ++x) {
+                                        float v = __uint_as_float(0x7fc00000u);                  // (8 bits: a scale that stands for NaN)
+                                        if (!E4M3)
+                                            v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.c.v.ptr)[page * p.c.v.sb + m.h * p.c.v.sh + (t % p.c.P) * p.c.v.st + q * 16 + x]);
+                                        if (j < nvis) ov[x] = __float_as_uint(fmaf(wt, v, __uint_as_float(ov[x])));
+                                    }
+                                    tc_st16(tO + q * 16, ov);
+                                }
+                                tc_wait_st();
+                            }
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::PFULL + w));
+                }
+            }
+            base += c.n;
+            if (fail_site) break;
+            // ---- the segment's result ----
+            if (cnt > 0) {
+                if (!wait(L::ODONE + w, no, __LINE__)) break;
+                ++no;
+                tc_fence_after();
+            }
+            const bool whole = seg.whole(), there = r < m.rows;
+            const float k = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
+            int head = 0, iq = 0;
+            if (there) row_place(p, m, r, head, iq);
+            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + iq * p.o.st;
+            const size_t at = seg.slot() * kChunkRows + r;
+            if (cnt > 0 || whole) {
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t ov[32];
+                    if (cnt > 0) {
+                        tc_ld32(tO + q * 32, ov);
+                        tc_wait_ld32(ov);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) ov[j] = 0u;
+                    }
+                    if (!there) continue;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        float f[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(ov[j + x]) * k;
+                        if (whole) {
+                            *reinterpret_cast<uint4*>(dst + q * 32 + j) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+                        } else {
+                            float4* po = reinterpret_cast<float4*>(p.part_o + at * kD + q * 32 + j);
+                            po[0] = make_float4(f[0], f[1], f[2], f[3]);
+                            po[1] = make_float4(f[4], f[5], f[6], f[7]);
+                        }
+                    }
+                }
+            }
+            if (there && whole && p.lse) p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + iq] = lse_of(m_used == -INFINITY ? 0.f : m_used, l);
+            if (there && !whole) { p.part_m[at] = m_used; p.part_l[at] = l; }
+            tc_fence_before();                                      // (O is read: the next segment's MMAs follow the next P's barrier)
+            if (threadIdx.x == 128) note_item<kChunkRows>(p, run, seg);
+        }
+    } else {
+        // ======================= 8-bit codes -> bf16 tiles, the row's scale multiplied in =======================
+        fewer_registers<L::kOtherRegs>();
+        const int row = threadIdx.x - 384, sw = row & 7;
+        Segments<kChunkRows> seg(p, run);
+        uint32_t n = 0;
+        while (!fail_site && seg.next()) {
+            const ChunkSeg c = chunk_seg(p, seg);
+            for (int i = 0; i < c.n && !fail_site; ++i) {
+                const int t = (seg.ta + i) * kTokTile + row;
+                for (int op = 0; op < 2; ++op, ++n) {
+                    const uint32_t st = n & 1, slot = n % NS;
+                    if (!wait(L::RAWFULL + st, n >> 1, __LINE__)) break;
+                    const uint8_t* raw = smem + L::kRawAt + st * 16384u + row * 128;
+                    uint4 x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(raw + ((j ^ sw) << 4));
+                    const uint32_t s = smem[L::kScales + st * 128u + row];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::RAWEMPTY + st));
+                    // code bits are the value times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range
+                    const bool nan = s > 186u, odd = op && nan && t >= c.first_masked && t < seg.m.len, gone = op && (odd || t >= seg.m.len);
+                    const int e1 = min((int)s - 7, 127), e2 = (int)s - 7 - e1;
+                    const __nv_bfloat16 f1 = nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
+                    const __nv_bfloat16 f2 = __float2bfloat16(__uint_as_float((uint32_t)(min(e2, 127) + 127) << 23));
+                    const __nv_bfloat162 m1 = __halves2bfloat162(f1, f1), m2 = __halves2bfloat162(f2, f2);
+                    if (!wait(L::EMPTY + slot, (n / NS) ^ 1u, __LINE__)) break;
+                    uint8_t* dst = smem + L::kRing + slot * kOperandBytes + row * 128;
+                    const bool two = __any_sync(0xffffffffu, e2 > 0);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {                  // 8 channels at a time
+                        uint4 y;
+                        codes_to_bf16(j & 1 ? x[j >> 1].z : x[j >> 1].x, m1, m2, two, y.x, y.y);
+                        codes_to_bf16(j & 1 ? x[j >> 1].w : x[j >> 1].y, m1, m2, two, y.z, y.w);
+                        if (gone) y = make_uint4(0u, 0u, 0u, 0u);
+                        *reinterpret_cast<uint4*>(dst + (j >> 3) * kHalfBytes + (((j & 7) ^ sw) << 4)) = y;
+                    }
+                    const uint32_t word = __ballot_sync(0xffffffffu, odd);
+                    if (op && lane == 0) bad_words[slot * 4 + (warp - 12)] = word;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::FULL + slot));
+                }
+            }
+        }
+    }
+    if (fail_site) atomicCAS(p.status, 0u, (unsigned)fail_site);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+}  // namespace
+}  // namespace obc

@@ -52,6 +52,15 @@ __device__ __forceinline__ int seen_by(const AttnParams& p, const Item& m, int r
     return p.causal ? min(max(m.len - m.ql + (m.r0 + r) / p.G + 1, 0), m.len) : m.len;
 }
 
+// four e4m3 codes as the low and the high bytes of bf16 numbers: their bits, shifted into bf16's fields, stand for the value times 2^-120
+// (subnormal codes included)
+__device__ __forceinline__ void expand(uint32_t x, uint32_t& lo, uint32_t& hi) {
+    lo = (x << 4) & 0xf0f0f0f0u;
+    hi = (x & 0x80808080u) | ((x >> 4) & 0x07070707u);
+}
+// natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)
+__device__ __forceinline__ float lse_of(float ref, float total) { return (ref + log2f(total)) * 0.6931471805599453f; }
+
 struct Run { long long begin, end, total, ctas; int item, off; };
 struct RunScratch { long long warp_sum[32]; Run run; };
 

@@ -240,3 +240,59 @@ def test_long_list_behind_32_bits():
     ko, vo = api.obc_paged_read(L.cache, n_tokens=1000)
     assert torch.equal(ko[:, :, 700:], new) and torch.equal(vo[:, :, 700:], new)
     assert torch.equal(ko[:, :, :700].double(), L.k[:, :, :700])
+
+
+# ---- chunks: more than 32 rows per list --------------------------------------------------------------------------
+
+CHUNK_BITS = {"f32": 22, "bf16": 8, "e4m3": 8}       # weights in one bf16
+
+
+@pytest.mark.parametrize("pages", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("T,Hq,H,lens,P", [
+    (33, 1, 1, [33], 16), (40, 4, 2, [100, 40], 8), (128, 1, 1, [128], 16), (129, 1, 1, [200], 24), (64, 8, 2, [700, 64, 129], 32), (37, 7, 1, [1000], 128),
+    (256, 2, 2, [256], 16), (257, 1, 1, [1025], 40), (300, 4, 1, [300, 513], 64), (700, 2, 1, [701], 16), (5, 8, 1, [2000, 6], 16), (90, 28, 4, [90], 256),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunks(pages, T, Hq, H, lens, P, causal):
+    _attend(Lists(lens, H, P, pages, seed=T), Hq, T, causal=causal, weight_bits=CHUNK_BITS[pages])
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+def test_long_chunks(pages):
+    """Items that many CTAs share, items that one CTA finishes, and both in one run."""
+    _attend(Lists([9000, 300], 2, 16, pages, seed=1), 8, 200, weight_bits=8)
+    _attend(Lists([2500], 8, 64, pages, seed=2), 16, 900, weight_bits=8)
+    _attend(Lists([700] * 20, 8, 16, pages, seed=3), 8, 100, weight_bits=8)
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+def test_chunks_of_a_padded_batch(pages):
+    L = Lists([900, 1, 0, 260, 64, 500], 2, 16, pages, seed=6)
+    _attend(L, 8, 260, q_lens=[260, 1, 0, 260, 100, 1], weight_bits=8)         # single tokens beside chunks; more queries than tokens
+    _attend(L, 8, 260, q_lens=[1, 260, 260, 0, -3, 999], causal=False, scale=0.2, weight_bits=8)
+    _attend(Lists([[150, 20], [33, 640]], 2, 16, pages, by_head=True, seed=7, strided=True), 8, 50, q_lens=[50, 33], strided_q=True, weight_bits=8)
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("spread", [2, 12])
+def test_chunks_of_different_magnitude(pages, spread):
+    _attend(Lists([700, 77], 2, 16, pages, seed=1, spread=spread), 8, 60, weight_bits=8)
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+@pytest.mark.parametrize("n,T", [(300, 100), (140, 140), (1100, 300)])
+def test_infinities_and_nan_in_chunks(pages, what, n, T):
+    """Rows of V that are not finite, at places that all, some and the last queries see, in tiles of one and of two warpgroups."""
+    g = torch.Generator().manual_seed(n)
+    k, v = torch.randn((1, 2, n, D), generator=g), torch.randn((1, 2, n, D), generator=g)
+    first = n - T
+    for t, ch in ((first + T // 2, 5), (first + T // 2 + 1, 6), (n - 1, 7), (first + 1, 8)):
+        v[0, 0, t, ch] = what
+    L = Lists([n], 2, 16, pages, seed=1, k=k, v=v)
+    _attend(L, 4, T, weight_bits=8)
+    k[0, 1, first + T // 3] = math.nan
+    L = Lists([n], 2, 16, pages, seed=1, k=k, v=v)
+    q = torch.randn((1, 4, T, D), generator=_gen(3), device="cuda").bfloat16()
+    o, lse = api.obc_paged_attention(q, L.cache)
+    assert torch.isfinite(o[:, 2:, :T // 3]).all() and torch.isnan(o[:, 2:, T // 3:]).all() and torch.isnan(lse[:, 2:, T // 3:]).all()
