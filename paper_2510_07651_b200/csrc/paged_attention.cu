@@ -195,7 +195,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             if (++tile == seg.tb) { more = seg.next(); tile = seg.ta; }
             if (more) page = page_at();                             // the next tile's page numbers travel meanwhile
             const int st = n % L::kStages;
-            if (!mbar_wait(empty(st), ((n / L::kStages) & 1) ^ 1)) { fail_site = __LINE__; break; }
+            if (!__all_sync(0xffffffffu, mbar_wait(empty(st), ((n / L::kStages) & 1) ^ 1))) { fail_site = __LINE__; break; }
             few_issue<E4M3>(p, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(st), lane, pg, h, t0);
             ++n;
         }
@@ -249,7 +249,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 const int st = n % L::kStages;
                 uint8_t* sk = smem + st * L::kStage;
                 uint8_t* sv = sk + L::kOperand;
-                if (!mbar_wait(full(st), (n / L::kStages) & 1)) { fail_site = __LINE__; break; }
+                if (!__all_sync(0xffffffffu, mbar_wait(full(st), (n / L::kStages) & 1))) { fail_site = __LINE__; break; }
                 const int t0 = tile * kTokTile + tok0;              // the warp's first token
                 const bool edge = t0 + 16 > first_masked;           // some row does not see some of the 16 tokens
                 float s[MT][2][4];

@@ -6,14 +6,14 @@
 //     O_w += P_w V_i                         A operand from TMEM, V as MN-major B
 // While one warpgroup is at its exponentials the MMAs of the other run; a K or V tile is fetched once for both.  m_w only moves when a
 // tile's maximum exceeds it by more than 2^8, so that O_w is rescaled (in TMEM, by the thread that owns the row) a few times per
-// list.  MMAs issued by one thread execute in order: S_w(i+1) cannot overwrite P_w(i) before P_w V(i) has read it, and the
+// list.  The MMAs of a warpgroup are issued by one thread and execute in order: S_w(i+1) cannot overwrite P_w(i) before P_w V(i) has read it, and the
 // commit behind S_w(i+1) covers P_w V(i).
 //
 //   warp 0       producer: pages -> ring of 32 KB operands (K and V tiles in turn); 8-bit pages -> ring of raw tiles and their scales
-//   warp 1       MMA issuer
-//   warps 2-3    Q of the next segment; warp 2: V tiles at a list's end: rows behind it become zeros, rows that are not finite and that not
+//   warps 1, 3   MMA issuers, one for each softmax warpgroup (one thread for both was what set the pace)
+//   warp 2       V tiles at a list's end: rows behind it become zeros, rows that are not finite and that not
 //                every query sees become zeros, too, and are named to the softmax warps, which add them by hand where they are seen
-//   warps 4-11   softmax, two warpgroups
+//   warps 4-11   softmax, two warpgroups; each fetches its Q
 //   warps 12-15  (8-bit pages) codes -> bf16 tiles, the scale multiplied in exactly; and what warp 2 does for V tiles
 // TMEM columns: S_0 [0,128)  S_1 [128,256)  O_0 [256,384)  O_1 [384,512)
 #pragma once
@@ -33,7 +33,7 @@ template <bool E4M3> struct ChunkLayout {
     static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
     static constexpr uint32_t kBad = kScales + kRaw * 128u;                            // [slot][4] words: tokens to be added by hand
     static constexpr uint32_t kBars = kBad + kSlots * 16u;
-    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, QEMPTY, SFULL, PFULL = SFULL + 2, ODONE = PFULL + 2, RAWFULL = ODONE + 2,
+    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PFULL = SFULL + 2, ODONE = PFULL + 2, RAWFULL = ODONE + 2,
            RAWEMPTY = RAWFULL + 2, NBARS = RAWEMPTY + 2 };
     static constexpr uint32_t kTmem = kBars + NBARS * 8u;
     static constexpr uint32_t kSmem = kTmem + 16 + 1024;
@@ -90,10 +90,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
-        for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 1); mbar_init(bar(L::EDGE + i), 1); }
-        mbar_init(bar(L::QFULL), 64); mbar_init(bar(L::QEMPTY), 1);
+        for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 2); mbar_init(bar(L::EDGE + i), 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
+            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
             mbar_init(bar(L::RAWFULL + i), 33); mbar_init(bar(L::RAWEMPTY + i), 4);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -112,6 +111,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     int fail_site = 0;
     auto wait = [&](int b, uint32_t parity, int line) -> bool {
         if (mbar_wait(bar(b), parity & 1u)) return true;
+        fail_site = line;
+        return false;
+    };
+    // (for whole warps that go on together: where one lane gave up all do)
+    auto all_wait = [&](int b, uint32_t parity, int line) -> bool {
+        if (__all_sync(0xffffffffu, wait(b, parity, line))) return true;
         fail_site = line;
         return false;
     };
@@ -142,7 +147,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const CUtensorMap* map = op ? &map_v : &map_k;
                     if (E4M3) {
                         const uint32_t st = n & 1, full = bar(L::RAWFULL + st);
-                        if (!wait(L::RAWEMPTY + st, (n >> 1) ^ 1u, __LINE__)) break;
+                        if (!all_wait(L::RAWEMPTY + st, (n >> 1) ^ 1u, __LINE__)) break;
                         if (lane == 0) mbar_expect_tx(full, 16384);
                         __syncwarp();
                         if (lane < boxes) tma_load_4d(sbase + L::kRawAt + st * 16384u + lane * p.box * 128, map, full, 0, slot, hh, pg);
@@ -154,7 +159,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
                     } else {
                         const uint32_t st = n % NS, full = bar((op && edge ? L::EDGE : L::FULL) + st);
-                        if (!wait(L::EMPTY + st, (n / NS) ^ 1u, __LINE__)) break;
+                        if (!all_wait(L::EMPTY + st, (n / NS) ^ 1u, __LINE__)) break;
                         if (lane == 0) mbar_expect_tx(full, kOperandBytes);
                         __syncwarp();
                         if (lane < boxes) {
@@ -171,92 +176,70 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 const uint32_t k = n - 1 - back;
                 (void)mbar_wait(bar((E4M3 ? (int)L::RAWFULL : (int)L::FULL) + k % ring), (k / ring) & 1u);
             }
-        } else if (warp == 1) {
-            // ===================================== MMA issuer =======================================
+        } else if (warp & 1) {
+            // ===================================== MMA issuers ======================================
             if (lane == 0) {
+                const int w = warp >> 1;
                 const uint32_t idesc_s = idesc_bf16(kTokTile);
                 const uint32_t idesc_pv = idesc_bf16(kD) | (1u << 16);           // B operand (V) is MN-major
+                const uint32_t aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes), tS = tmem + w * 128u, tO = tmem + 256u + w * 128u;
                 Segments<kChunkRows> seg(p, run);
-                uint32_t base = 0, np[2] = {0, 0}, q_n = 0;                      // tiles before this segment; P tiles taken; segments
+                uint32_t base = 0, np = 0, nq = 0;                               // tiles before this segment; P tiles taken; Q tiles taken
                 while (!fail_site && seg.next()) {
                     const ChunkSeg c = chunk_seg(p, seg);
+                    const int cnt = c.cnt(w);
                     auto slot_of = [&](int i, int op) { return (2 * (base + i) + op) % NS; };
                     auto full = [&](int i, int op, int line) { return wait(L::FULL + slot_of(i, op), (2 * (base + i) + op) / NS, line); };
-                    auto issue_s = [&](int w, int i) {
-                        const uint32_t ak = desc_lo_k(sbase + L::kRing + slot_of(i, 0) * kOperandBytes), aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes);
+                    // S(i), or, past the tiles that this warpgroup sees, its word that K(i) may go
+                    auto step_s = [&](int i) -> bool {
+                        if (!full(i, 0, __LINE__)) return false;
+                        const int ks0 = slot_of(i, 0);
+                        if (i >= cnt) { mbar_arrive(bar(L::EMPTY + ks0)); return true; }
+                        tc_fence_after();
+                        const uint32_t ak = desc_lo_k(sbase + L::kRing + ks0 * kOperandBytes);
 #pragma unroll
                         for (int ks = 0; ks < 8; ++ks)
-                            tc_mma(tmem + w * 128u, desc_make(aq + desc_kstep(ks, kHalfBytes)), desc_make(ak + desc_kstep(ks, kHalfBytes)), idesc_s, ks > 0);
+                            tc_mma(tS, desc_make(aq + desc_kstep(ks, kHalfBytes)), desc_make(ak + desc_kstep(ks, kHalfBytes)), idesc_s, ks > 0);
                         tc_commit(bar(L::SFULL + w));
+                        tc_commit(bar(L::EMPTY + ks0));
+                        return true;
                     };
-                    if (!wait(L::QFULL, q_n, __LINE__) || !full(0, 0, __LINE__)) break;
-                    ++q_n;
-                    tc_fence_after();
-                    if (c.cnt0 > 0) issue_s(0, 0);
-                    if (c.cnt1 > 0) issue_s(1, 0);
-                    tc_commit(bar(L::EMPTY + slot_of(0, 0)));
-                    if (c.n == 1) tc_commit(bar(L::QEMPTY));
-                    for (int i = 0; i < c.n && !fail_site; ++i) {
+                    if (cnt > 0 && !wait(L::QFULL + w, nq++, __LINE__)) break;
+                    if (!step_s(0)) break;
+                    for (int i = 0; i < c.n; ++i) {
                         const int vs = slot_of(i, 1);
                         if (!full(i, 1, __LINE__)) break;
-                        const int last = i < c.cnt1 ? 1 : 0;                 // the last warpgroup that reads V_i
+                        if (i < cnt) {
+                            if (!wait(L::PFULL + w, np++, __LINE__)) break;
+                            tc_fence_after();
+                            const uint32_t av = desc_lo_mn(sbase + L::kRing + vs * kOperandBytes);
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            if (i < c.cnt(w)) {
-                                if (!wait(L::PFULL + w, np[w], __LINE__)) break;
-                                ++np[w];
-                                tc_fence_after();
-                                const uint32_t av = desc_lo_mn(sbase + L::kRing + vs * kOperandBytes);
-#pragma unroll
-                                for (int ks = 0; ks < 8; ++ks)           // 128 tokens = 8 steps of K = 16 (2048 bytes of V each)
-                                    tc_mma_ts(tmem + 256u + w * 128u, tmem + w * 128u + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
-                                if (w == last) tc_commit(bar(L::EMPTY + vs));
-                                if (i == c.cnt(w) - 1) tc_commit(bar(L::ODONE + w));
-                            }
-                            if (i + 1 < c.cnt(w)) {
-                                if (!full(i + 1, 0, __LINE__)) break;
-                                issue_s(w, i + 1);
-                            }
+                            for (int ks = 0; ks < 8; ++ks)               // 128 tokens = 8 steps of K = 16 (2048 bytes of V each)
+                                tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
+                            tc_commit(bar(L::EMPTY + vs));
+                            if (i == cnt - 1) tc_commit(bar(L::ODONE + w));
+                        } else {
+                            mbar_arrive(bar(L::EMPTY + vs));
                         }
-                        if (fail_site) break;
-                        if (i + 1 < c.n) {
-                            tc_commit(bar(L::EMPTY + slot_of(i + 1, 0)));
-                            if (i + 2 == c.n) tc_commit(bar(L::QEMPTY));
-                        }
+                        if (i + 1 < c.n && !step_s(i + 1)) break;
                     }
                     base += c.n;
                 }
             }
         } else {
-            // ======================= Q tiles; V tiles at the end of what is seen =======================
-            const int t64 = threadIdx.x - 64;
-            Segments<kChunkRows> seg(p, run);
-            uint32_t base = 0, q_n = 0, edges = 0;
-            while (!fail_site && seg.next()) {
-                const Item& m = seg.m;
-                const ChunkSeg c = chunk_seg(p, seg);
-                if (!wait(L::QEMPTY, q_n ^ 1u, __LINE__)) break;
-                ++q_n;
-                const int rows = m.rows > 128 ? 256 : 128, piece = t64 & 15;
-#pragma unroll 4
-                for (int r = t64 >> 4; r < rows; r += 4) {          // sixteen lanes per row; rows that are not there become zeros
-                    int head = 0, i = 0;
-                    if (r < m.rows) row_place(p, m, r, head, i);
-                    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.ptr) + m.b * p.q.sb + head * p.q.sh + i * p.q.st + piece * 8;
-                    const int rr = r & 127;
-                    const uint32_t dst = sbase + L::kQ + (r >> 7) * kOperandBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4);
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(r < m.rows ? 16 : 0) : "memory");
-                }
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                fence_async_smem();
-                mbar_arrive(bar(L::QFULL));
-                if (!E4M3 && warp == 2) {
+            // ======================= V tiles at the end of what is seen =======================
+            if (!E4M3) {
+                Segments<kChunkRows> seg(p, run);
+                uint32_t base = 0, edges = 0;
+                while (!fail_site && seg.next()) {
+                    const Item& m = seg.m;
+                    const ChunkSeg c = chunk_seg(p, seg);
                     for (int i = 0; i < c.n; ++i) {
                         const int t0 = (seg.ta + i) * kTokTile;
                         if (!is_edge(c, t0)) continue;
                         const uint32_t op = 2 * (base + i) + 1;
                         const int vs = op % NS;
-                        if (!wait(L::EDGE + vs, edges >> vs, __LINE__)) break;
+                        if (!all_wait(L::EDGE + vs, edges >> vs, __LINE__)) break;
                         edges ^= 1u << vs;
                         uint8_t* tile = smem + L::kRing + vs * kOperandBytes;
 #pragma unroll 1
@@ -282,8 +265,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         __syncwarp();
                         if (lane == 0) mbar_arrive(bar(L::FULL + vs));
                     }
+                    base += c.n;
                 }
-                base += c.n;
             }
         }
     } else if (warp < 12) {
@@ -293,10 +276,30 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         const uint32_t lane_addr = (uint32_t)(lane_grp * 32) << 16;
         const uint32_t tS = tmem + lane_addr + w * 128u, tO = tmem + lane_addr + 256u + w * 128u;
         const float2 sl2v = make_float2(p.sl2, p.sl2);
+        // Q of a segment: sixteen lanes per row; rows that are not there become zeros.  Asked for as soon as the segment before has its last logits.
+        auto ask_q = [&](const Item& m) {
+            const int tid = lane_grp * 32 + lane, piece = tid & 15;
+#pragma unroll 4
+            for (int rr = tid >> 4; rr < 128; rr += 8) {
+                const bool there = w * 128 + rr < m.rows;
+                int head = 0, i = 0;
+                if (there) row_place(p, m, w * 128 + rr, head, i);
+                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.ptr) + (there ? m.b * p.q.sb + head * p.q.sh + i * p.q.st : 0) + piece * 8;
+                const uint32_t dst = sbase + L::kQ + w * kOperandBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+            }
+        };
+        auto q_there = [&]() {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_smem();
+            mbar_arrive(bar(L::QFULL + w));
+        };
         Segments<kChunkRows> seg(p, run);
         uint32_t base = 0, ns = 0, no = 0;
-        while (!fail_site && seg.next()) {
-            const Item& m = seg.m;
+        bool more = seg.next();
+        if (more && chunk_seg(p, seg).cnt(w) > 0) { ask_q(seg.m); q_there(); }
+        while (more && !fail_site) {
+            const Item m = seg.m;
             const ChunkSeg c = chunk_seg(p, seg);
             const int cnt = c.cnt(w), seen = seen_by(p, m, r);
             float m_used = -INFINITY, l = 0.f;
@@ -312,7 +315,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 const int t0 = (seg.ta + i) * kTokTile, vs = (2 * (base + i) + 1) % NS;
                 const bool edge = is_edge(c, t0);
                 if (i < cnt) {
-                    if (!wait(L::SFULL + w, ns, __LINE__)) break;
+                    if (!all_wait(L::SFULL + w, ns, __LINE__)) break;
                     ++ns;
                     tc_fence_after();
                     uint32_t s[128];
@@ -372,7 +375,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tc_wait_st();
                     if (edge) {                                     // rows of V that are added by hand
-                        if (!wait(L::FULL + vs, (2 * (base + i) + 1) / NS, __LINE__)) break;
+                        if (!all_wait(L::FULL + vs, (2 * (base + i) + 1) / NS, __LINE__)) break;
 #pragma unroll 1
                         for (int b = 0; b < 4; ++b) {
                             uint32_t word = bad_words[vs * 4 + b];
@@ -409,18 +412,22 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             }
             base += c.n;
             if (fail_site) break;
+            const bool whole = seg.whole(), there = r < m.rows;
+            const size_t at = seg.slot() * kChunkRows + r;
+            if (threadIdx.x == 128) note_item<kChunkRows>(p, run, seg);
+            more = seg.next();
+            const bool next_q = more && chunk_seg(p, seg).cnt(w) > 0;
+            if (next_q) ask_q(seg.m);
             // ---- the segment's result ----
             if (cnt > 0) {
-                if (!wait(L::ODONE + w, no, __LINE__)) break;
+                if (!all_wait(L::ODONE + w, no, __LINE__)) break;
                 ++no;
                 tc_fence_after();
             }
-            const bool whole = seg.whole(), there = r < m.rows;
             const float k = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
             int head = 0, iq = 0;
             if (there) row_place(p, m, r, head, iq);
             __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + iq * p.o.st;
-            const size_t at = seg.slot() * kChunkRows + r;
             if (cnt > 0 || whole) {
 #pragma unroll 1
                 for (int q = 0; q < 4; ++q) {
@@ -451,7 +458,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (there && whole && p.lse) p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + iq] = lse_of(m_used == -INFINITY ? 0.f : m_used, l);
             if (there && !whole) { p.part_m[at] = m_used; p.part_l[at] = l; }
             tc_fence_before();                                      // (O is read: the next segment's MMAs follow the next P's barrier)
-            if (threadIdx.x == 128) note_item<kChunkRows>(p, run, seg);
+            if (next_q) q_there();
         }
     } else {
         // ======================= 8-bit codes -> bf16 tiles, the row's scale multiplied in =======================
@@ -465,12 +472,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 const int t = (seg.ta + i) * kTokTile + row;
                 for (int op = 0; op < 2; ++op, ++n) {
                     const uint32_t st = n & 1, slot = n % NS;
-                    if (!wait(L::RAWFULL + st, n >> 1, __LINE__)) break;
+                    if (!all_wait(L::RAWFULL + st, n >> 1, __LINE__)) break;
                     const uint8_t* raw = smem + L::kRawAt + st * 16384u + row * 128;
                     uint4 x[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(raw + ((j ^ sw) << 4));
                     const uint32_t s = smem[L::kScales + st * 128u + row];
+                    // (the loads above may still be under way, and nothing below uses them soon: without the fence the bulk copy that the
+                    // arrival lets go has been seen to overtake them)
+                    fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::RAWEMPTY + st));
                     // code bits are the value times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range
@@ -479,7 +489,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const __nv_bfloat16 f1 = nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
                     const __nv_bfloat16 f2 = __float2bfloat16(__uint_as_float((uint32_t)(min(e2, 127) + 127) << 23));
                     const __nv_bfloat162 m1 = __halves2bfloat162(f1, f1), m2 = __halves2bfloat162(f2, f2);
-                    if (!wait(L::EMPTY + slot, (n / NS) ^ 1u, __LINE__)) break;
+                    if (!all_wait(L::EMPTY + slot, (n / NS) ^ 1u, __LINE__)) break;
                     uint8_t* dst = smem + L::kRing + slot * kOperandBytes + row * 128;
                     const bool two = __any_sync(0xffffffffu, e2 > 0);
 #pragma unroll
