@@ -33,7 +33,7 @@ template <bool E4M3> struct ChunkLayout {
     static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
     static constexpr uint32_t kBad = kScales + kRaw * 128u;                            // [slot][4] words: tokens to be added by hand
     static constexpr uint32_t kBars = kBad + kSlots * 16u;
-    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PFULL = SFULL + 2, ODONE = PFULL + 2, RAWFULL = ODONE + 2,
+    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PHALF = SFULL + 2, PFULL = PHALF + 2, TURN = PFULL + 2, ODONE = TURN + 8, RAWFULL = ODONE + 2,
            RAWEMPTY = RAWFULL + 2, NBARS = RAWEMPTY + 2 };
     static constexpr uint32_t kTmem = kBars + NBARS * 8u;
     static constexpr uint32_t kSmem = kTmem + 16 + 1024;
@@ -59,6 +59,13 @@ __device__ __forceinline__ ChunkSeg chunk_seg(const AttnParams& p, const Segment
     return c;
 }
 
+// a value that all lanes of the warp have, known as such
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void tc_ld1(uint32_t taddr, uint32_t& r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
 }
@@ -87,14 +94,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     auto bar = [&](int i) { return sbase + L::kBars + 8u * (uint32_t)i; };
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + L::kTmem);
     uint32_t* bad_words = reinterpret_cast<uint32_t*>(smem + L::kBad);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
         for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 2); mbar_init(bar(L::EDGE + i), 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
+            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PHALF + i), 4); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
             mbar_init(bar(L::RAWFULL + i), 33); mbar_init(bar(L::RAWEMPTY + i), 4);
         }
+        for (int i = 0; i < 8; ++i) mbar_init(bar(L::TURN + i), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -104,7 +112,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = uniform(*tmem_slot);
     pdl_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0u;        // no wait of this call can have given up yet (each lasts seconds)
     const Run run = find_run<kChunkRows>(p, &scratch);
@@ -178,53 +186,69 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             }
         } else if (warp & 1) {
             // ===================================== MMA issuers ======================================
-            if (lane == 0) {
-                const int w = warp >> 1;
-                const uint32_t idesc_s = idesc_bf16(kTokTile);
-                const uint32_t idesc_pv = idesc_bf16(kD) | (1u << 16);           // B operand (V) is MN-major
-                const uint32_t aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes), tS = tmem + w * 128u, tO = tmem + 256u + w * 128u;
-                Segments<kChunkRows> seg(p, run);
-                uint32_t base = 0, np = 0, nq = 0;                               // tiles before this segment; P tiles taken; Q tiles taken
-                while (!fail_site && seg.next()) {
-                    const ChunkSeg c = chunk_seg(p, seg);
-                    const int cnt = c.cnt(w);
-                    auto slot_of = [&](int i, int op) { return (2 * (base + i) + op) % NS; };
-                    auto full = [&](int i, int op, int line) { return wait(L::FULL + slot_of(i, op), (2 * (base + i) + op) / NS, line); };
-                    // S(i), or, past the tiles that this warpgroup sees, its word that K(i) may go
-                    auto step_s = [&](int i) -> bool {
-                        if (!full(i, 0, __LINE__)) return false;
-                        const int ks0 = slot_of(i, 0);
-                        if (i >= cnt) { mbar_arrive(bar(L::EMPTY + ks0)); return true; }
+            // The whole warp walks the loop and one lane issues: slots and addresses are then uniform values, which the instruction takes as they
+            // are (issued from a loop of one thread each MMA cost the moves of its descriptors, too).
+            const int w = warp >> 1;
+            const bool leader = elect_one();
+            const uint32_t idesc_s = idesc_bf16(kTokTile);
+            const uint32_t idesc_pv = idesc_bf16(kD) | (1u << 16);               // B operand (V) is MN-major
+            const uint32_t aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes), tS = tmem + w * 128u, tO = tmem + 256u + w * 128u;
+            Segments<kChunkRows> seg(p, run);
+            uint32_t op = 0, slot = 0, phase = 0, np = 0, nq = 0;                // operand, its slot and round; P tiles taken; Q tiles taken
+            auto next_op = [&]() { ++op; if (++slot == NS) { slot = 0; phase ^= 1u; } };
+            while (seg.next()) {
+                const ChunkSeg c = chunk_seg(p, seg);
+                const int n = uniform(c.n), cnt = uniform(c.cnt(w));
+                // S(i), or, past the tiles that this warpgroup sees, its word that K(i) may go
+                auto step_s = [&](int i) -> bool {
+                    if (!all_wait(L::FULL + slot, phase, __LINE__)) return false;
+                    if (i < cnt) {
                         tc_fence_after();
-                        const uint32_t ak = desc_lo_k(sbase + L::kRing + ks0 * kOperandBytes);
+                        if (leader) {
+                            const uint32_t ak = desc_lo_k(sbase + L::kRing + slot * kOperandBytes);
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks)
-                            tc_mma(tS, desc_make(aq + desc_kstep(ks, kHalfBytes)), desc_make(ak + desc_kstep(ks, kHalfBytes)), idesc_s, ks > 0);
-                        tc_commit(bar(L::SFULL + w));
-                        tc_commit(bar(L::EMPTY + ks0));
-                        return true;
-                    };
-                    if (cnt > 0 && !wait(L::QFULL + w, nq++, __LINE__)) break;
-                    if (!step_s(0)) break;
-                    for (int i = 0; i < c.n; ++i) {
-                        const int vs = slot_of(i, 1);
-                        if (!full(i, 1, __LINE__)) break;
-                        if (i < cnt) {
-                            if (!wait(L::PFULL + w, np++, __LINE__)) break;
-                            tc_fence_after();
-                            const uint32_t av = desc_lo_mn(sbase + L::kRing + vs * kOperandBytes);
-#pragma unroll
-                            for (int ks = 0; ks < 8; ++ks)               // 128 tokens = 8 steps of K = 16 (2048 bytes of V each)
-                                tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
-                            tc_commit(bar(L::EMPTY + vs));
-                            if (i == cnt - 1) tc_commit(bar(L::ODONE + w));
-                        } else {
-                            mbar_arrive(bar(L::EMPTY + vs));
+                            for (int ks = 0; ks < 8; ++ks)
+                                tc_mma(tS, desc_make(aq + desc_kstep(ks, kHalfBytes)), desc_make(ak + desc_kstep(ks, kHalfBytes)), idesc_s, ks > 0);
+                            tc_commit(bar(L::SFULL + w));
+                            tc_commit(bar(L::EMPTY + slot));
                         }
-                        if (i + 1 < c.n && !step_s(i + 1)) break;
+                    } else if (leader) {
+                        mbar_arrive(bar(L::EMPTY + slot));
                     }
-                    base += c.n;
+                    __syncwarp();
+                    next_op();
+                    return true;
+                };
+                if (cnt > 0 && !all_wait(L::QFULL + w, nq++, __LINE__)) break;
+                if (!step_s(0)) break;
+                for (int i = 0; i < n; ++i) {
+                    if (!all_wait(L::FULL + slot, phase, __LINE__)) break;
+                    if (i < cnt) {
+                        const uint32_t av = desc_lo_mn(sbase + L::kRing + slot * kOperandBytes);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {                            // 64 tokens of P at a time, as they come
+                            if (!all_wait((h ? L::PFULL : L::PHALF) + w, np, __LINE__)) break;
+                            tc_fence_after();
+                            if (leader) {
+#pragma unroll
+                                for (int ks = 4 * h; ks < 4 * h + 4; ++ks)       // steps of K = 16 tokens (2048 bytes of V each)
+                                    tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
+                            }
+                        }
+                        if (fail_site) break;
+                        ++np;
+                        if (leader) {
+                            tc_commit(bar(L::EMPTY + slot));
+                            if (i == cnt - 1) tc_commit(bar(L::ODONE + w));
+                        }
+                    } else if (leader) {
+                        mbar_arrive(bar(L::EMPTY + slot));
+                    }
+                    __syncwarp();
+                    next_op();
+                    if (i + 1 < n && !step_s(i + 1)) break;
                 }
+                if (fail_site) break;
             }
         } else {
             // ======================= V tiles at the end of what is seen =======================
@@ -295,13 +319,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             mbar_arrive(bar(L::QFULL + w));
         };
         Segments<kChunkRows> seg(p, run);
-        uint32_t base = 0, ns = 0, no = 0;
+        uint32_t base = 0, ns = 0, no = 0, turns = 0;
         bool more = seg.next();
         if (more && chunk_seg(p, seg).cnt(w) > 0) { ask_q(seg.m); q_there(); }
         while (more && !fail_site) {
             const Item m = seg.m;
             const ChunkSeg c = chunk_seg(p, seg);
-            const int cnt = c.cnt(w), seen = seen_by(p, m, r);
+            const int cnt = c.cnt(w), both = min(c.cnt0, c.cnt1), seen = seen_by(p, m, r), ta = seg.ta;
             float m_used = -INFINITY, l = 0.f;
             if (cnt > 0) {                                          // O starts at 0 (all of its MMAs accumulate)
                 uint32_t z[32];
@@ -311,10 +335,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 for (int q = 0; q < 4; ++q) tc_st32(tO + q * 32, z);
                 tc_wait_st();                                       // (ordered before the MMAs by the first P's barrier)
             }
-            for (int i = 0; i < c.n; ++i) {
-                const int t0 = (seg.ta + i) * kTokTile, vs = (2 * (base + i) + 1) % NS;
+            for (int i = 0; i < cnt; ++i) {
+                const int t0 = (ta + i) * kTokTile;
                 const bool edge = is_edge(c, t0);
-                if (i < cnt) {
+                {
                     if (!all_wait(L::SFULL + w, ns, __LINE__)) break;
                     ++ns;
                     tc_fence_after();
@@ -359,6 +383,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const float m_eff = m_used == -INFINITY ? 0.f : m_used;
                     const float2 negm = make_float2(-m_eff, -m_eff);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    // The two warps of an SM sub-partition take turns at the exponentials, one per warpgroup: left alone they run side by side, and then
+                    // wait side by side for their MMAs.  (Warpgroup 0 begins; its turn k follows turn k - 1 of warpgroup 1.)
+                    if (i < both) {
+                        if ((w == 1 || turns > 0) && !all_wait(L::TURN + 4 * w + lane_grp, w ? turns : turns - 1u, __LINE__)) break;
+                        ++turns;
+                    }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t pk[16];
@@ -371,11 +401,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             pk[j >> 1] = pack_bf16x2(ex.x, ex.y);
                         }
                         tc_st16(tS + q * 16, pk);
+                        if (q == 1 && !edge) {                      // the MMAs may have the first 64 tokens
+                            tc_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(bar(L::PHALF + w));
+                        }
                     }
+                    if (i < both && lane == 0) mbar_arrive(bar(L::TURN + 4 * (w ^ 1) + lane_grp));
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tc_wait_st();
                     if (edge) {                                     // rows of V that are added by hand
-                        if (!all_wait(L::FULL + vs, (2 * (base + i) + 1) / NS, __LINE__)) break;
+                        const uint32_t vop = 2 * (base + i) + 1, vs = vop % NS;
+                        if (!all_wait(L::FULL + vs, vop / NS, __LINE__)) break;
 #pragma unroll 1
                         for (int b = 0; b < 4; ++b) {
                             uint32_t word = bad_words[vs * 4 + b];
@@ -407,7 +445,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(L::PFULL + w));
+                    if (lane == 0) {
+                        if (edge) mbar_arrive(bar(L::PHALF + w));
+                        mbar_arrive(bar(L::PFULL + w));
+                    }
                 }
             }
             base += c.n;
