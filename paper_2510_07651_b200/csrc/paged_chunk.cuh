@@ -69,7 +69,6 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void tc_ld1(uint32_t taddr, uint32_t& r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0x7f80u) == 0x7f80u || (bf16x2 & 0x7f800000u) == 0x7f800000u; }
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 // four bytes (e4m3 codes) -> two bf16 pairs, times m1 * m2 (powers of two that leave the product exact)
@@ -320,6 +319,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         };
         Segments<kChunkRows> seg(p, run);
         uint32_t base = 0, ns = 0, no = 0, turns = 0;
+        int4 info = make_int4(-1, 0, 0, 0);
         bool more = seg.next();
         if (more && chunk_seg(p, seg).cnt(w) > 0) { ask_q(seg.m); q_there(); }
         while (more && !fail_site) {
@@ -455,7 +455,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (fail_site) break;
             const bool whole = seg.whole(), there = r < m.rows;
             const size_t at = seg.slot() * kChunkRows + r;
-            if (threadIdx.x == 128) note_item<kChunkRows>(p, run, seg);
+            info = seg.shared_item(run);
             more = seg.next();
             const bool next_q = more && chunk_seg(p, seg).cnt(w) > 0;
             if (next_q) ask_q(seg.m);
@@ -501,6 +501,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             tc_fence_before();                                      // (O is read: the next segment's MMAs follow the next P's barrier)
             if (next_q) q_there();
         }
+        if (threadIdx.x == 128) p.info[blockIdx.x] = info;
     } else {
         // ======================= 8-bit codes -> bf16 tiles, the row's scale multiplied in =======================
         fewer_registers<L::kOtherRegs>();

@@ -1,11 +1,13 @@
 // What the kernels of obc_paged_attention share: how the work is cut into pieces, and where partial results go.
 //
 // An item is a tile of `ROWS` query rows of one KV list (row r = i G + g is query i of the group's head g, so that a tile's rows are near
-// one another in position and stop at the same tokens).  An item costs as many token tiles of 128 as its last row sees.  All items, in
-// order, are cut into a run of equal cost per CTA, so that ragged batches, lists per head and causal chunks load every CTA alike
-// whatever the lengths, which only the device knows.  A CTA's run is a sequence of segments, each a range of tiles of one item.  An
-// item that lies within one run is finished there; the others leave partial results (maximum, sum, unnormalised output) that the
-// merge kernel joins in the order of the tiles.  A run has at most two such segments, its first and its last.
+// one another in position and stop at the same tokens).  An item costs as many token tiles of 128 as its last row sees, and kSegCost tiles'
+// time for its beginning and end.  All items, in order, are cut into a run of equal cost per CTA, so that ragged batches, lists per
+// head and causal chunks load every CTA alike whatever the lengths, which only the device knows.  (Without the constant the CTA with
+// the shortest items of a 4096-token prompt took half again as long as the others.)  A CTA's run is a sequence of segments, each a
+// range of tiles of one item.  An item that lies within one run is finished there; the others leave partial results (maximum, sum,
+// unnormalised output) that the merge kernel joins in the order of the tiles.  A run has at most two such segments, its first
+// and its last, and an item that is shared is the last one of the CTA that it begins in: the merge goes by these CTAs.
 #pragma once
 #include "obc_common.cuh"
 
@@ -24,7 +26,7 @@ struct AttnParams {
     int nrt, items;                          // row tiles per list, items in all
     int box, one_head;                       // tokens per bulk copy; pages of one head
     unsigned int* status;                    // workspace header: source line of the wait that gave up
-    int4* info;                              // per item: first and last CTA and the first one's slot; x < 0: finished by one CTA
+    int4* info;                              // per CTA: the shared item that begins in it (or -1), the item's last CTA, its slot here
     float *part_m, *part_l, *part_o;         // [2 gridDim][ROWS] (x d): slots of a CTA's first and last segment
 };
 
@@ -58,8 +60,12 @@ __device__ __forceinline__ void expand(uint32_t x, uint32_t& lo, uint32_t& hi) {
     lo = (x << 4) & 0xf0f0f0f0u;
     hi = (x & 0x80808080u) | ((x >> 4) & 0x07070707u);
 }
+// infinity or NaN in either half
+__device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0x7f80u) == 0x7f80u || (bf16x2 & 0x7f800000u) == 0x7f800000u; }
 // natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)
 __device__ __forceinline__ float lse_of(float ref, float total) { return (ref + log2f(total)) * 0.6931471805599453f; }
+
+constexpr int kSegCost = 2;
 
 struct Run { long long begin, end, total, ctas; int item, off; };
 struct RunScratch { long long warp_sum[32]; Run run; };
@@ -69,8 +75,9 @@ template <int ROWS>
 __device__ __forceinline__ Run find_run(const AttnParams& p, RunScratch* s) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nwarps = blockDim.x >> 5;
     const int per = (p.items + blockDim.x - 1) / blockDim.x, i0 = tid * per, i1 = min(i0 + per, p.items);
+    auto cost = [&](int i) { const int n = item_of<ROWS>(p, i).tiles; return n > 0 ? n + kSegCost : 0; };
     long long mine = 0;
-    for (int i = i0; i < i1; ++i) mine += item_of<ROWS>(p, i).tiles;
+    for (int i = i0; i < i1; ++i) mine += cost(i);
     long long scan = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -92,7 +99,7 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, RunScratch* s) {
     if (begin >= before && begin < before + mine) {
         long long at = before;
         for (int i = i0; i < i1; ++i) {
-            const int n = item_of<ROWS>(p, i).tiles;
+            const int n = cost(i);
             if (begin < at + n) { s->run.item = i; s->run.off = (int)(begin - at); break; }
             at += n;
         }
@@ -105,40 +112,33 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, RunScratch* s) {
 template <int ROWS>
 struct Segments {
     const AttnParams& p;
-    long long at, end;
-    int next_item, off;
+    long long at, end;                       // where the next item begins; the run's end
+    int next_item, off;                      // off: what of the next item's cost lies before the run
     Item m;                                  // the segment: tiles [ta, tb) of item `item`
     int item, ta, tb;
     bool first;
-    __device__ __forceinline__ Segments(const AttnParams& p_, const Run& r) : p(p_), at(r.begin), end(r.end), next_item(r.item), off(r.off), first(true) { item = -1; }
+    __device__ __forceinline__ Segments(const AttnParams& p_, const Run& r) : p(p_), at(r.begin - r.off), end(r.end), next_item(r.item), off(r.off), first(true) { item = -1; }
     __device__ __forceinline__ bool next() {
         if (item >= 0) first = false;
-        if (at >= end) return false;
-        for (;; ++next_item) {
-            m = item_of<ROWS>(p, next_item);
-            if (m.tiles > 0) break;
+        while (at + off < end) {
+            m = item_of<ROWS>(p, next_item++);
+            if (m.tiles == 0) continue;
+            ta = max(off - kSegCost, 0);
+            tb = (int)max(min(end - at - kSegCost, (long long)m.tiles), 0ll);
+            at += m.tiles + kSegCost;
+            off = 0;
+            if (ta < tb) { item = next_item - 1; return true; }
         }
-        item = next_item; ta = off;
-        tb = (int)min((long long)m.tiles, off + (end - at));
-        at += tb - ta;
-        ++next_item; off = 0;
-        return true;
+        return false;
     }
     __device__ __forceinline__ bool whole() const { return ta == 0 && tb == m.tiles; }
     __device__ __forceinline__ size_t slot() const { return 2 * (size_t)blockIdx.x + (first ? 0 : 1); }
-};
-
-// the CTA that an item begins in says how it is shared out
-template <int ROWS>
-__device__ __forceinline__ void note_item(const AttnParams& p, const Run& r, const Segments<ROWS>& s) {
-    if (s.ta != 0) return;
-    int4 v = make_int4(-1, -1, 0, 0);
-    if (!s.whole()) {
-        const long long last = s.at - (s.tb - s.ta) + s.m.tiles - 1;          // the item's last tile
-        v = make_int4((int)blockIdx.x, (int)(((last + 1) * r.ctas + r.total - 1) / r.total) - 1, s.first ? 0 : 1, 0);
+    // of the current segment, for the merge
+    __device__ __forceinline__ int4 shared_item(const Run& r) const {
+        if (ta != 0 || tb == m.tiles) return make_int4(-1, 0, 0, 0);
+        return make_int4(item, (int)((at * r.ctas + r.total - 1) / r.total) - 1, first ? 0 : 1, 0);        // at - 1: the item's last tile
     }
-    p.info[s.item] = v;
-}
+};
 
 // where the row (i G + g) of an item's list stands in q, o and lse
 __device__ __forceinline__ void row_place(const AttnParams& p, const Item& m, int r, int& head, int& i) {

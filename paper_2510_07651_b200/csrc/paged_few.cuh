@@ -1,0 +1,445 @@
+// Attention of at most 16 rows per KV list (single tokens of a GQA group, a few tokens of a small one) over a paged cache.
+//
+// Bound by the K and V bytes.  Pages arrive as bulk copies (TMA) in a ring of 128-token tiles; a warp takes 16 tokens of a tile and runs
+// warp-level MMAs with the tokens on the M side, so that the (at most 8 per step) rows lie on N and nothing is padded to more:
+//     S^T = K q^T      16 tokens x 8 rows, 8 steps of 16 channels
+//     O^T += V^T P^T   16 channels x 8 rows, 8 tiles, one step of 16 tokens; P^T is S^T's accumulator turned by movmatrix
+// A warp keeps (m, l, O) of its own tokens; they meet once per segment.  P enters as bf16(P) + bf16(P - bf16(P)), so that o is off by no
+// more than its own rounding (the MMAs are nowhere near their limit here).  What sets the pace is the chain of dependent steps of a warp
+// per tile, hence two groups of eight warps on alternate tiles where the registers allow it (8 rows).
+//
+// e4m3 rows are expanded in registers: the code's bits, shifted into bf16's fields, are the value times 2^-120 (subnormals included).  The
+// channels of a 16-channel step are taken in the order in which ldmatrix hands out their bytes (q is loaded in the same order), and the
+// rows of an O^T tile are eight even and eight odd channels.  2^60 goes into q; the scale of a K row, 2^60 and the rest of 2^120 into
+// its logit, that of a V row and 2^60 into its P, and the last 2^60 into the result.
+#pragma once
+#include "paged_common.cuh"
+#include "tc_ptx.cuh"
+#include "warp_mma.cuh"
+
+namespace obc {
+namespace {
+
+template <int NT, bool E4M3> struct FewLayout {
+    static constexpr int kRows = 8 * NT, kGroups = NT == 1 ? 2 : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 32;
+    static constexpr uint32_t kOperand = kTokTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
+    static constexpr int kStages = E4M3 ? 5 : 3, kFull = kStages * kGroups;
+    static constexpr int kPitch = kD + 4;                                                  // floats per row of O in the merge buffer
+    static constexpr uint32_t kMerge = kStages * kStage, kMergeBytes = 8 * 8 * kPitch * 4;
+    static constexpr uint32_t kScales = kMerge + kMergeBytes;                              // [stage][K, V][128] scale bytes
+    static constexpr uint32_t kBars = kScales + (E4M3 ? (uint32_t)kStages * 256u : 0u);    // full, empty
+    static constexpr uint32_t kSmem = kBars + (kFull + kStages) * 8u + 1024;               // + alignment slack
+};
+
+// (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3), of four codes as bf16 pairs, each value times 2^-120
+__device__ __forceinline__ void expand_adjacent(uint32_t x, uint32_t& p01, uint32_t& p23) {
+    uint32_t lo, hi;
+    expand(x, lo, hi);
+    p01 = __byte_perm(lo, hi, 0x5140); p23 = __byte_perm(lo, hi, 0x7362);
+}
+__device__ __forceinline__ void expand_alternate(uint32_t x, uint32_t& p02, uint32_t& p13) {
+    uint32_t lo, hi;
+    expand(x, lo, hi);
+    p02 = __byte_perm(lo, hi, 0x6240); p13 = __byte_perm(lo, hi, 0x7351);
+}
+// B operand of step ks from one row of q: channels 16 ks + 2 c, + 1 and + 8, + 9; e4m3: 16 ks + 4 c, .. + 3, times 2^60.  nullptr: zeros.
+template <bool E4M3>
+__device__ __forceinline__ void q_fragment(uint32_t (&b)[2], const __nv_bfloat16* src, int ks, int c) {
+    if (E4M3) {
+        const uint2 u = src ? *reinterpret_cast<const uint2*>(src + ks * 16 + c * 4) : make_uint2(0u, 0u);
+        const __nv_bfloat162 up = __floats2bfloat162_rn(0x1p60f, 0x1p60f);
+        const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u.x), up), y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u.y), up);
+        b[0] = *reinterpret_cast<const uint32_t*>(&x); b[1] = *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(src);
+        b[0] = u ? u[ks * 8 + c] : 0u; b[1] = u ? u[ks * 8 + 4 + c] : 0u;
+    }
+}
+// an 8x8 tile of 16-bit values turned: the lane's pair (row lane / 4, columns 2 (lane % 4), + 1) becomes that of the transpose
+__device__ __forceinline__ uint32_t turned(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+// barriers of the consumer warps
+template <int N> __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory"); }
+template <int N> __device__ __forceinline__ bool consumers_or(bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)x), "n"(N) : "memory");
+    return r != 0;
+}
+// 2^(s - 67): a row's scale with the 2^60 that is due beside it
+__device__ __forceinline__ float scale_60(uint32_t s) { return __uint_as_float(s > 186u ? 0x7fc00000u : (s + 60u) << 23); }
+
+// Copies the tile's pages (and scales) into a stage; all lanes of a warp.  `page`: of the lane's box, -1 for rows of zeros.
+template <typename L, bool E4M3>
+__device__ __forceinline__ void few_issue(const AttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, uint32_t stage, uint32_t scales, uint32_t bar,
+                                          int lane, int page, int h, int t0) {
+    if (lane == 0) mbar_expect_tx(bar, L::kStage);
+    __syncwarp();
+    const int n = kTokTile / p.box, slot = (t0 + lane * p.box) % p.c.P, hh = p.one_head ? 0 : h;
+    if (lane < n) {
+        const uint32_t d = stage + lane * p.box * 128;
+        tma_load_4d(d, mk, bar, 0, slot, hh, page);
+        if (!E4M3) tma_load_4d(d + kHalfBytes, mk, bar, 64, slot, hh, page);
+        tma_load_4d(d + L::kOperand, mv, bar, 0, slot, hh, page);
+        if (!E4M3) tma_load_4d(d + L::kOperand + kHalfBytes, mv, bar, 64, slot, hh, page);
+    }
+    if (E4M3) {                              // 8 scale bytes per lane: lanes 0-15 K, 16-31 V
+        const int t8 = (lane & 15) * 8, pg = __shfl_sync(0xffffffffu, page, t8 / p.box);
+        const uint8_t* base = lane < 16 ? p.c.ks : p.c.vs;
+        const uint8_t* src = base + (pg < 0 ? 0ll : pg * p.c.ss_p + h * p.c.ss_h + (t0 + t8) % p.c.P);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(scales + (lane >> 4) * 128 + t8), "l"(src), "r"(pg < 0 ? 0 : 8) : "memory");
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
+    }
+}
+
+template <int NT, bool E4M3>
+__global__ void __launch_bounds__(FewLayout<NT, E4M3>::kThreads, 1)
+few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnParams p) {
+    using L = FewLayout<NT, E4M3>;
+    constexpr int ROWS = L::kRows, CONS = 32 * L::kWarps;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t sbase = smem_u32(smem);
+    __shared__ RunScratch scratch;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // Tile n of the CTA goes through stage n mod kStages and announces itself on barrier n mod kFull: a stage has a barrier for each group, since
+    // a group waits for every other tile only and could not tell by its parity how often a barrier that it had not watched has turned.
+    auto full = [&](int i) { return sbase + L::kBars + 8u * (uint32_t)i; };
+    auto empty = [&](int i) { return sbase + L::kBars + 8u * (uint32_t)(L::kFull + i); };
+    if (threadIdx.x == 0) {
+        prefetch_tmap(&map_k); prefetch_tmap(&map_v);
+        for (int i = 0; i < L::kFull; ++i) mbar_init(full(i), E4M3 ? 33 : 1);
+        for (int i = 0; i < L::kStages; ++i) mbar_init(empty(i), 8);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0u;        // no wait of this call can have given up yet (each lasts seconds)
+    const Run run = find_run<ROWS>(p, &scratch);                    // (its barriers also publish the mbarriers)
+    int fail_site = 0;
+    Segments<ROWS> seg(p, run);
+
+    if (warp == L::kWarps) {
+        // ===================================== producer =====================================
+        bool more = seg.next();
+        int tile = seg.ta;
+        auto page_at = [&]() -> int {                               // the lane's box of the current tile
+            const int t = tile * kTokTile + lane * p.box;
+            return lane < kTokTile / p.box && t < seg.m.len ? p.c.page_of(seg.m.b, seg.m.h, t) : -1;
+        };
+        int page = more ? page_at() : -1;
+        int n = 0, st = 0, fb = 0;                                  // tiles issued; stage and barrier of the next
+        uint32_t phase = 1;
+        while (more) {
+            const int pg = page, h = seg.m.h, t0 = tile * kTokTile;
+            if (++tile == seg.tb) { more = seg.next(); tile = seg.ta; }
+            if (more) page = page_at();                             // the next tile's page numbers travel meanwhile
+            if (!__all_sync(0xffffffffu, mbar_wait(empty(st), phase))) { fail_site = __LINE__; break; }
+            few_issue<L, E4M3>(p, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(fb), lane, pg, h, t0);
+            ++n;
+            if (++fb == L::kFull) fb = 0;
+            if (++st == L::kStages) { st = 0; phase ^= 1u; }
+        }
+        for (int back = 0; back < L::kStages && back < n; ++back) { // no copy may be under way when the CTA leaves
+            const int k = n - 1 - back;
+            (void)mbar_wait(full(k % L::kFull), (k / L::kFull) & 1);
+        }
+    } else {
+        // ===================================== consumers ====================================
+        const int g = lane >> 2, c = lane & 3, group = warp >> 3, wg = warp & 7;
+        const int tok0 = wg * 16;                                   // the warp's tokens of a tile
+        int4 info = make_int4(-1, 0, 0, 0);
+        int st = 0, fb = 0, turn = 0;                               // stage, barrier and group of the next tile
+        uint32_t phase = 0;
+        while (seg.next()) {
+            const Item m = seg.m;
+            info = seg.shared_item(run);
+            uint32_t qf[NT][8][2];
+            int seen[NT][2];                                        // of rows 2 c, 2 c + 1
+            float mx[NT][2], l[NT][2];
+            float o[NT][8][4];                                      // O^T: channel tile; (row g, columns 2 c, 2 c + 1), (row g + 8, ..)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const __nv_bfloat16* src = nullptr;
+                if (nt * 8 + g < m.rows) {
+                    int head, i;
+                    row_place(p, m, nt * 8 + g, head, i);
+                    src = static_cast<const __nv_bfloat16*>(p.q.ptr) + m.b * p.q.sb + head * p.q.sh + i * p.q.st;
+                }
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) q_fragment<E4M3>(qf[nt][ks], src, ks, c);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) { seen[nt][j] = seen_by(p, m, nt * 8 + 2 * c + j); mx[nt][j] = -INFINITY; l[nt][j] = 0.f; }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { o[nt][j][0] = 0.f; o[nt][j][1] = 0.f; o[nt][j][2] = 0.f; o[nt][j][3] = 0.f; }
+            }
+            const int first_masked = p.causal ? min(max(m.len - m.ql + m.r0 / p.G + 1, 0), m.len) : m.len;   // tokens that not every row sees begin here
+
+            for (int tile = seg.ta; tile < seg.tb; ++tile) {
+                const bool mine = L::kGroups == 1 || turn == group;
+                const int s_at = st, f_at = fb;
+                const uint32_t par = phase;
+                turn ^= 1;
+                if (++st == L::kStages) st = 0;
+                if (++fb == L::kFull) { fb = 0; phase ^= 1u; }
+                if (!mine) continue;
+                uint8_t* sk = smem + s_at * L::kStage;
+                uint8_t* sv = sk + L::kOperand;
+                if (!__all_sync(0xffffffffu, mbar_wait(full(f_at), par))) { fail_site = __LINE__; break; }
+                const int t0 = tile * kTokTile + tok0;              // the warp's first token
+                const bool edge = t0 + 16 > first_masked;           // some row does not see some of the 16 tokens
+                if (t0 < m.len) {
+                    float s[NT][4], s2[NT][4];                      // even and odd steps: half the chain
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { s[nt][j] = 0.f; s2[nt][j] = 0.f; }
+                    const int a_row = tok0 + (lane & 15), a_pc = lane >> 4;      // tiles in A's order: (tokens 0-7, p), (8-15, p), (0-7, p + 1), (8-15, p + 1)
+                    if (E4M3) {
+#pragma unroll
+                        for (int pc = 0; pc < 8; pc += 2) {
+                            uint32_t r[4];
+                            ldsm_x4(r, sk + a_row * 128 + (((pc + a_pc) ^ (a_row & 7)) << 4));
+                            uint32_t a[4], b[4];
+                            expand_adjacent(r[0], a[0], a[2]); expand_adjacent(r[1], a[1], a[3]);
+                            expand_adjacent(r[2], b[0], b[2]); expand_adjacent(r[3], b[1], b[3]);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_bf16(s[nt], a, qf[nt][pc][0], qf[nt][pc][1]);
+                                mma_bf16(s2[nt], b, qf[nt][pc + 1][0], qf[nt][pc + 1][1]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks) {
+                            const int piece = 2 * ks + a_pc;
+                            uint32_t a[4];
+                            ldsm_x4(a, sk + (piece >> 3) * kHalfBytes + a_row * 128 + (((piece & 7) ^ (a_row & 7)) << 4));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) mma_bf16(ks & 1 ? s2[nt] : s[nt], a, qf[nt][ks][0], qf[nt][ks][1]);
+                        }
+                    }
+                    float fk[2] = {p.sl2, p.sl2}, fv[2] = {1.f, 1.f};            // factors of the lane's tokens g and g + 8
+                    if (E4M3) {
+                        const uint8_t* sc = smem + L::kScales + s_at * 256 + tok0 + g;
+                        fk[0] = scale_60(sc[0]) * p.sl2; fk[1] = scale_60(sc[8]) * p.sl2;
+                        fv[0] = scale_60(sc[128]); fv[1] = scale_60(sc[136]);
+                    }
+                    uint32_t ph[NT][2], pl[NT][2];                  // P^T as B operands: high and low parts
+                    float e[NT][4];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float tm[2];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            float x = (s[nt][j] + s2[nt][j]) * fk[j >> 1];
+                            if (edge && t0 + g + 8 * (j >> 1) >= seen[nt][j & 1]) x = -INFINITY;
+                            s[nt][j] = x;
+                        }
+                        tm[0] = fmaxf(s[nt][0], s[nt][2]); tm[1] = fmaxf(s[nt][1], s[nt][3]);
+                        // the reference moves only when the maximum exceeds it by 2^8 (P stays far inside fp32's and bf16's range): first asked
+                        // of every lane's own two tokens, so that most tiles need no exchange
+                        if (__any_sync(0xffffffffu, tm[0] > mx[nt][0] + 8.f || tm[1] > mx[nt][1] + 8.f)) {
+                            float f[2];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                                for (int w = 4; w < 32; w <<= 1) tm[j] = fmaxf(tm[j], __shfl_xor_sync(0xffffffffu, tm[j], w));
+                                f[j] = 1.f;
+                                if (tm[j] > mx[nt][j] + 8.f) { f[j] = exp2f(mx[nt][j] - tm[j]); mx[nt][j] = tm[j]; }
+                                l[nt][j] *= f[j];
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) { o[nt][j][0] *= f[0]; o[nt][j][1] *= f[1]; o[nt][j][2] *= f[0]; o[nt][j][3] *= f[1]; }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float ref = mx[nt][j & 1];
+                            const float x = fast_exp2(s[nt][j] - (ref == -INFINITY ? 0.f : ref));
+                            l[nt][j & 1] += x;
+                            e[nt][j] = E4M3 ? (x > 0.f ? x * fv[j >> 1] : x) : x;          // (a NaN logit stays NaN; a token not seen has weight 0 whatever its scale)
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            uint32_t hi, lo;
+                            split_bf16x2(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
+                            ph[nt][j] = turned(hi); pl[nt][j] = turned(lo);
+                        }
+                    }
+                    if (!E4M3 && edge) {
+                        // rows that not every query sees: those behind the list's end may hold anything and become zeros; one that
+                        // is not finite must reach the queries that see it alone
+                        bool odd = false;
+                        const int row = tok0 + (lane >> 1), t = t0 + (lane >> 1);
+                        uint4* at = reinterpret_cast<uint4*>(sv + (lane & 1) * kHalfBytes + row * 128);
+                        if (t >= m.len) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) at[j] = make_uint4(0u, 0u, 0u, 0u);
+                        } else if (t >= first_masked) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const uint4 u = at[j];
+                                odd |= not_finite(u.x) || not_finite(u.y) || not_finite(u.z) || not_finite(u.w);
+                            }
+                        }
+                        __syncwarp();
+                        unsigned bad = __ballot_sync(0xffffffffu, odd);
+                        while (bad) {                               // token by token, on CUDA cores; the row is zeroed for the MMAs
+                            const int tk = (__ffs(bad) - 1) >> 1, rw = tok0 + tk;
+                            bad &= ~(3u << (2 * tk));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                float w[2];
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    w[j] = __shfl_sync(0xffffffffu, tk & 8 ? e[nt][2 + j] : e[nt][j], (tk & 7) * 4 + c);
+                                    if (t0 + tk >= seen[nt][j]) continue;
+#pragma unroll
+                                    for (int x = 0; x < 16; ++x) {  // channels 8 x + g
+                                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(sv + (x >> 3) * kHalfBytes + rw * 128 + (((x & 7) ^ (rw & 7)) << 4) + g * 2);
+                                        o[nt][x >> 1][(x & 1) * 2 + j] += w[j] * __bfloat162float(v);
+                                    }
+                                }
+                            }
+                            __syncwarp();
+                            if (lane < 16) *reinterpret_cast<uint4*>(sv + (lane >> 3) * kHalfBytes + rw * 128 + ((lane & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                            __syncwarp();
+                        }
+                    }
+                    const int v_row = tok0 + (lane & 7) + (lane >> 4) * 8, v_pc = (lane >> 3) & 1;   // (tokens 0-7, p), (0-7, p + 1), (8-15, p), (8-15, p + 1)
+                    if (E4M3) {
+#pragma unroll
+                        for (int pc = 0; pc < 8; pc += 2) {
+                            uint32_t r[4], a[4], b[4];
+                            ldsm_x4_trans(r, sv + v_row * 128 + (((pc + v_pc) ^ (v_row & 7)) << 4));
+                            expand_alternate(r[0], a[0], a[1]); expand_alternate(r[2], a[2], a[3]);      // piece pc: even channels, odd channels
+                            expand_alternate(r[1], b[0], b[1]); expand_alternate(r[3], b[2], b[3]);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_bf16(o[nt][pc], a, ph[nt][0], ph[nt][1]);
+                                mma_bf16(o[nt][pc + 1], b, ph[nt][0], ph[nt][1]);
+                                mma_bf16(o[nt][pc], a, pl[nt][0], pl[nt][1]);
+                                mma_bf16(o[nt][pc + 1], b, pl[nt][0], pl[nt][1]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int piece = 2 * j + v_pc;
+                            uint32_t a[4];
+                            ldsm_x4_trans(a, sv + (piece >> 3) * kHalfBytes + v_row * 128 + (((piece & 7) ^ (v_row & 7)) << 4));
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_bf16(o[nt][j], a, ph[nt][0], ph[nt][1]);
+                                mma_bf16(o[nt][j], a, pl[nt][0], pl[nt][1]);
+                            }
+                        }
+                    }
+                }
+                if (edge && !E4M3) fence_async_smem();              // this thread's writes to the stage precede the bulk copy into it
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty(s_at));
+            }
+
+            // ---- the warps' results meet: maxima and sums, then O, eight rows at a time ----
+            float* sm = reinterpret_cast<float*>(smem + L::kMerge);            // [warp][ROWS] maxima, then sums
+            float* sl = sm + L::kWarps * ROWS;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int w = 4; w < 32; w <<= 1) l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], w);
+                    if (g == 0) { sm[warp * ROWS + nt * 8 + 2 * c + j] = mx[nt][j]; sl[warp * ROWS + nt * 8 + 2 * c + j] = l[nt][j]; }
+                }
+            if (consumers_or<CONS>(fail_site != 0)) {               // one warp's wait gave up: all leave
+                if (!fail_site) fail_site = __LINE__;
+                break;
+            }
+            // the reference and the sum of a row over all warps
+            auto joined = [&](int r, float& ref, float& total) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < L::kWarps; ++w) top = fmaxf(top, sm[w * ROWS + r]);
+                ref = top == -INFINITY ? 0.f : top;
+                total = 0.f;
+#pragma unroll
+                for (int w = 0; w < L::kWarps; ++w) total = fmaf(exp2f(sm[w * ROWS + r] - ref), sl[w * ROWS + r], total);
+            };
+            float f[NT][2], ref_w[NT], sum_w[NT];                   // factors of the lane's rows; statistics of row 8 nt + wg
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < L::kWarps; ++w) top = fmaxf(top, sm[w * ROWS + nt * 8 + 2 * c + j]);
+                    f[nt][j] = exp2f(mx[nt][j] - (top == -INFINITY ? 0.f : top));
+                }
+                joined(nt * 8 + wg, ref_w[nt], sum_w[nt]);
+            }
+            const bool whole = seg.whole();
+            float* buf = reinterpret_cast<float*>(smem + L::kMerge);           // [warp of the group][row][channel]
+            auto put = [&](int nt) {
+                float* at = buf + wg * 8 * L::kPitch + 2 * c * L::kPitch;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int ch = 16 * j + (E4M3 ? 2 * g : g), up = E4M3 ? 1 : 8;
+                    at[ch] = o[nt][j][0] * f[nt][0]; at[L::kPitch + ch] = o[nt][j][1] * f[nt][1];
+                    at[ch + up] = o[nt][j][2] * f[nt][0]; at[L::kPitch + ch + up] = o[nt][j][3] * f[nt][1];
+                }
+            };
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt * 8 >= m.rows) break;
+                consumers_sync<CONS>();                             // the buffer is free (again)
+                if (L::kGroups == 2) {                              // the second group's first, added to by the first group in place
+                    if (group == 1) put(nt);
+                    consumers_sync<CONS>();
+                    if (group == 0) {
+                        float* at = buf + wg * 8 * L::kPitch + 2 * c * L::kPitch;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int ch = 16 * j + (E4M3 ? 2 * g : g), up = E4M3 ? 1 : 8;
+                            at[ch] += o[nt][j][0] * f[nt][0]; at[L::kPitch + ch] += o[nt][j][1] * f[nt][1];
+                            at[ch + up] += o[nt][j][2] * f[nt][0]; at[L::kPitch + ch + up] += o[nt][j][3] * f[nt][1];
+                        }
+                    }
+                } else {
+                    put(nt);
+                }
+                consumers_sync<CONS>();
+                // a warp of the first group sums and stores one row
+                const int r = nt * 8 + wg;
+                if (group != 0 || r >= m.rows) continue;
+                float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    const float4 x = *reinterpret_cast<const float4*>(buf + (w * 8 + wg) * L::kPitch + lane * 4);
+                    a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                }
+                const float sum = sum_w[nt], k = (E4M3 ? 0x1p60f : 1.f) * (whole ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
+                a.x *= k; a.y *= k; a.z *= k; a.w *= k;
+                if (whole) {
+                    int head, i;
+                    row_place(p, m, r, head, i);
+                    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + i * p.o.st;
+                    *reinterpret_cast<uint2*>(dst + lane * 4) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+                    if (p.lse && lane == 0) p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + i] = lse_of(ref_w[nt], sum);
+                } else {
+                    const size_t at = seg.slot() * ROWS + r;
+                    *reinterpret_cast<float4*>(p.part_o + at * kD + lane * 4) = a;
+                    if (lane == 0) { p.part_m[at] = sum == 0.f ? -INFINITY : ref_w[nt]; p.part_l[at] = sum; }
+                }
+            }
+            consumers_sync<CONS>();                                 // the buffer is free for the next segment's statistics
+        }
+        if (threadIdx.x == 0) p.info[blockIdx.x] = info;
+    }
+    if (fail_site && lane == 0) atomicCAS(p.status, 0u, (unsigned)fail_site);
+}
+
+}  // namespace
+}  // namespace obc

@@ -155,7 +155,8 @@ def _attend(L, Hq, T, *, q_lens=None, causal=True, scale=0.0, seed=9, weight_bit
     return q, o, lse
 
 
-BITS = {"f32": 22, "bf16": 15, "e4m3": 15}           # weights of few rows: two bf16 parts
+BITS = {"f32": 22, "bf16": 15, "e4m3": 15}           # weights of up to 16 rows per list: two bf16 parts
+CHUNK_BITS = {"f32": 22, "bf16": 8, "e4m3": 8}       # of more rows: one bf16, off by half a step of 2^-7 at most
 
 
 @pytest.mark.parametrize("pages", ["f32", "bf16", "e4m3"])
@@ -171,7 +172,15 @@ def test_single_tokens(pages, lens, Hq, H, P):
 @pytest.mark.parametrize("T,Hq,H", [(2, 4, 1), (3, 7, 1), (4, 8, 2), (5, 8, 4), (16, 1, 1), (9, 6, 2), (32, 1, 1), (4, 8, 1)])
 @pytest.mark.parametrize("lens", [[33], [129, 64], [700]])
 def test_few_rows(pages, T, Hq, H, lens):
-    _attend(Lists(lens, H, 16, pages, seed=T), Hq, T, weight_bits=BITS[pages])
+    _attend(Lists(lens, H, 16, pages, seed=T), Hq, T, weight_bits=(BITS if Hq // H * T <= 16 else CHUNK_BITS)[pages])
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq", [8, 16])
+def test_many_tiles_per_cta(pages, Hq):
+    """Rings that go round many times, lists that end inside a run and lists that many CTAs share."""
+    _attend(Lists([40000, 3, 9000, 130], 4, 64, pages, seed=1), Hq, 2, weight_bits=BITS[pages])
+    _attend(Lists([1500] * 40, 8, 16, pages, seed=2), Hq, 1, weight_bits=BITS[pages])
 
 
 @pytest.mark.parametrize("pages", ["bf16", "e4m3"])
@@ -242,10 +251,7 @@ def test_long_list_behind_32_bits():
     assert torch.equal(ko[:, :, :700].double(), L.k[:, :, :700])
 
 
-# ---- chunks: more than 32 rows per list --------------------------------------------------------------------------
-
-CHUNK_BITS = {"f32": 22, "bf16": 8, "e4m3": 8}       # weights in one bf16
-
+# ---- chunks: more than 16 rows per list --------------------------------------------------------------------------
 
 @pytest.mark.parametrize("pages", ["f32", "bf16", "e4m3"])
 @pytest.mark.parametrize("T,Hq,H,lens,P", [
