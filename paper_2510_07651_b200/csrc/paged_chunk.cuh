@@ -135,20 +135,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         fewer_registers<L::kOtherRegs>();
         if (warp == 0) {
             // ===================================== producer =====================================
-            Segments<kChunkRows> seg(p, run);
-            bool more = seg.next();
-            int tile = seg.ta;
-            auto page_at = [&]() -> int {                           // the lane's box of the current tile
-                const int t = tile * kTokTile + lane * p.box;
-                return lane < kTokTile / p.box && t < seg.m.len ? p.c.page_of(seg.m.b, seg.m.h, t) : -1;
-            };
-            int page = more ? page_at() : -1;
+            TileWalk<kChunkRows> walk(p, run, lane);
             uint32_t n = 0;                                         // operands issued
-            while (more && !fail_site) {
-                const int pg = page, h = seg.m.h, t0 = tile * kTokTile;
-                const bool edge = t0 + kTokTile > seen_by(p, seg.m, 0);
-                if (++tile == seg.tb) { more = seg.next(); tile = seg.ta; }
-                if (more) page = page_at();                         // the next tile's page numbers travel meanwhile
+            while (walk.more && !fail_site) {
+                const int pg = walk.page(), h = walk.cur.m.h, t0 = walk.tile * kTokTile;
+                const bool edge = t0 + kTokTile > seen_by(p, walk.cur.m, 0);
+                walk.advance();
                 const int boxes = kTokTile / p.box, slot = (t0 + lane * p.box) % p.c.P, hh = p.one_head ? 0 : h;
                 for (int op = 0; op < 2; ++op, ++n) {
                     const CUtensorMap* map = op ? &map_v : &map_k;

@@ -131,12 +131,62 @@ struct Segments {
         }
         return false;
     }
+    __device__ __forceinline__ void copy(const Segments& s) { at = s.at; end = s.end; next_item = s.next_item; off = s.off; m = s.m; item = s.item; ta = s.ta; tb = s.tb; first = s.first; }
     __device__ __forceinline__ bool whole() const { return ta == 0 && tb == m.tiles; }
     __device__ __forceinline__ size_t slot() const { return 2 * (size_t)blockIdx.x + (first ? 0 : 1); }
     // of the current segment, for the merge
     __device__ __forceinline__ int4 shared_item(const Run& r) const {
         if (ta != 0 || tb == m.tiles) return make_int4(-1, 0, 0, 0);
         return make_int4(item, (int)((at * r.ctas + r.total - 1) / r.total) - 1, first ? 0 : 1, 0);        // at - 1: the item's last tile
+    }
+};
+
+// The tiles of a CTA's run, for the warp that asks for their pages.  A lane holds the page number of one box in a window of 32
+// consecutive boxes (a tile has 128 / box <= 16 of them, so it lies within one window); the next window's, or the next segment's first,
+// travel while the current ones are used.  (With the numbers of one tile at a time, asked for one tile ahead, 32 sequences of up
+// to 8192 tokens took 124 us against 97 without any look-up.)
+template <int ROWS>
+struct TileWalk {
+    const AttnParams& p;
+    Segments<ROWS> cur, nxt;
+    bool more, more_next;
+    int lane, boxes, tile, pages, pages_next;
+    __device__ __forceinline__ TileWalk(const AttnParams& p_, const Run& r, int lane_) : p(p_), cur(p_, r), nxt(p_, r), lane(lane_) {
+        boxes = kTokTile / p.box;
+        more = cur.next();
+        nxt.next(); more_next = nxt.next();
+        tile = cur.ta;
+        pages = pages_next = -1;
+        if (more) { pages = asked(cur.m, window(tile)); ahead(); }
+    }
+    __device__ __forceinline__ int window(int t) const { return t * boxes >> 5; }
+    __device__ __forceinline__ int asked(const Item& m, int win) const {
+        const int t = (win * 32 + lane) * p.box;
+        int v = -1;
+        if (t < m.len) v = p.c.table[m.b * p.c.tb + m.h * p.c.th + t / p.c.P];
+        return v;
+    }
+    __device__ __forceinline__ void ahead() {
+        if (window(tile) < window(cur.tb - 1)) pages_next = asked(cur.m, window(tile) + 1);
+        else if (more_next) pages_next = asked(nxt.m, window(nxt.ta));
+    }
+    // page of the lane's box of the current tile; -1 for rows of zeros (behind the list, or a page that is not there)
+    __device__ __forceinline__ int page() const {
+        const int v = __shfl_sync(0xffffffffu, pages, (tile * boxes + lane) & 31);
+        return lane < boxes && (unsigned)v < (unsigned)p.c.n_pages ? v : -1;
+    }
+    __device__ __forceinline__ void advance() {
+        if (++tile < cur.tb) {
+            if (window(tile) != window(tile - 1)) { pages = pages_next; ahead(); }
+            return;
+        }
+        more = more_next;
+        if (!more) return;
+        cur.copy(nxt);
+        tile = cur.ta;
+        pages = pages_next;
+        more_next = nxt.next();
+        ahead();
     }
 };
 

@@ -119,23 +119,15 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0u;        // no wait of this call can have given up yet (each lasts seconds)
     const Run run = find_run<ROWS>(p, &scratch);                    // (its barriers also publish the mbarriers)
     int fail_site = 0;
-    Segments<ROWS> seg(p, run);
 
     if (warp == L::kWarps) {
         // ===================================== producer =====================================
-        bool more = seg.next();
-        int tile = seg.ta;
-        auto page_at = [&]() -> int {                               // the lane's box of the current tile
-            const int t = tile * kTokTile + lane * p.box;
-            return lane < kTokTile / p.box && t < seg.m.len ? p.c.page_of(seg.m.b, seg.m.h, t) : -1;
-        };
-        int page = more ? page_at() : -1;
+        TileWalk<ROWS> walk(p, run, lane);
         int n = 0, st = 0, fb = 0;                                  // tiles issued; stage and barrier of the next
         uint32_t phase = 1;
-        while (more) {
-            const int pg = page, h = seg.m.h, t0 = tile * kTokTile;
-            if (++tile == seg.tb) { more = seg.next(); tile = seg.ta; }
-            if (more) page = page_at();                             // the next tile's page numbers travel meanwhile
+        while (walk.more) {
+            const int pg = walk.page(), h = walk.cur.m.h, t0 = walk.tile * kTokTile;
+            walk.advance();
             if (!__all_sync(0xffffffffu, mbar_wait(empty(st), phase))) { fail_site = __LINE__; break; }
             few_issue<L, E4M3>(p, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(fb), lane, pg, h, t0);
             ++n;
@@ -150,6 +142,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         // ===================================== consumers ====================================
         const int g = lane >> 2, c = lane & 3, group = warp >> 3, wg = warp & 7;
         const int tok0 = wg * 16;                                   // the warp's tokens of a tile
+        Segments<ROWS> seg(p, run);
         int4 info = make_int4(-1, 0, 0, 0);
         int st = 0, fb = 0, turn = 0;                               // stage, barrier and group of the next tile
         uint32_t phase = 0;
