@@ -419,7 +419,8 @@ static obc_status resolve_pages(const obc_pages* c, PagesView* v) {
         if ((((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 7) != 0 || c->scale_stride_p % 8 || c->scale_stride_h % 8) return OBC_ERR_ALIGN;
         if (c->scale_stride_p < 0 || c->scale_stride_h < 0) return OBC_ERR_SHAPE;
     }
-    *v = PagesView{c->batch, c->n_kv_heads, c->n_pages, c->page_size, c->max_pages, c->max_pages * c->page_size, dtype,
+    *v = PagesView{c->batch, c->n_kv_heads, c->n_pages, c->page_size, c->max_pages, c->max_pages * c->page_size,
+                   FastDiv(c->page_size), FastDiv(c->n_kv_heads), dtype,
                    view(c->k), view(c->v), c->k_scale, c->v_scale, c->scale_stride_p, c->scale_stride_h,
                    c->table, c->table_stride_b, c->table_stride_h, c->lens, c->lens_stride_b, c->lens_stride_h};
     return OBC_OK;
@@ -462,7 +463,7 @@ static obc_status resolve_attention(const obc_pages* c, const obc_attention_para
     *s = AttnShape{p->n_q_heads, p->n_q_heads / c->n_kv_heads, p->n_tokens, p->q_lens, p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)kD), p->causal != 0};
     // rows of all lists, padded to the smallest tile, are counted in 32 bits
     if ((long long)c->batch * c->n_kv_heads * (((long long)s->G * s->T + 15) / 16 * 16) > 0x7fffffffLL) return OBC_ERR_SHAPE;
-    return OBC_OK;
+    return paged_attention_fits(*pv, *s) ? OBC_OK : OBC_ERR_SHAPE;
 }
 
 obc_status obc_paged_attention_workspace(const obc_pages* c, const obc_attention_params* p, size_t* bytes) {

@@ -136,9 +136,24 @@ obc_status launch_score_tc(const ScoreShape& s, TensorView q, TensorView k, Tens
                            float* scores, void* ws, cudaStream_t stream, const GivenAttention* given = nullptr,
                            SimtPlan* attention_only = nullptr);   // non-null: stop after pass 1 + combine, return the plan
 
+// Division of 0 <= n < 2^31 by a number that the host knows, as a multiplication by 2^(31 + s) / d rounded up (s: the bits of d - 1; the
+// error of the factor, below 2^-31 relative, cannot reach the next whole number).  An integer division is some 40 dependent
+// instructions, and the kernels of a paged cache start with several in a row.
+struct FastDiv {
+    uint32_t d = 1, m = 0, s = 0;
+    FastDiv() = default;
+    explicit FastDiv(int32_t by) : d((uint32_t)by) {
+        while ((1ull << s) < d) ++s;
+        m = (uint32_t)((1ull << (31 + s)) / d + 1);        // (d = 1 has no use for it)
+    }
+    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, m) >> (s - 1)); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+
 // ---- paged caches -----------------------------------------------------------------------------------
 struct PagesView {                       // a paged cache as the kernels see it
     int B, Hkv, n_pages, P, max_pages, max_len;
+    FastDiv by_P, by_H;                  // page of a token, batch item of a list
     int dtype;
     TensorView k, v;                     // sb: from page to page
     uint8_t *ks, *vs;
@@ -148,7 +163,7 @@ struct PagesView {                       // a paged cache as the kernels see it
     __device__ __forceinline__ int len(int b, int h) const { return min(max(lens[b * lb + h * lh], 0), max_len); }
     // page that holds token t of list (b, h); negative if the table names none
     __device__ __forceinline__ int page_of(int b, int h, int t) const {
-        const int page = table[b * tb + h * th + t / P];
+        const int page = table[b * tb + h * th + by_P.div(t)];
         return (unsigned)page < (unsigned)n_pages ? page : -1;
     }
 };
@@ -165,6 +180,7 @@ struct AttnShape {
     float scale;
     int causal;
 };
+bool paged_attention_fits(const PagesView& c, const AttnShape& s);      // tiles of all lists at their longest, counted in 32 bits
 size_t paged_attention_bytes(const PagesView& c, const AttnShape& s);
 obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, TensorView q, TensorView o, float* lse, void* ws, cudaStream_t stream);
 

@@ -107,10 +107,10 @@ paged_f32_kernel(const __grid_constant__ AttnParams p) {
             for (int u = 0; u < 8; ++u) {             // a warp fetches whole rows: token warp + 8 u
                 const int t = t0 + warp + 8 * u;
                 kx[u] = make_float4(0.f, 0.f, 0.f, 0.f); vx[u] = kx[u];
-                const int page = t < m.len ? p.c.page_of(m.b, m.h, t) : -1;
+                const int page = t < m.len ? p.c.page_of(m.b, m.h, t) : -1, slot = p.c.by_P.mod(t);
                 if (page >= 0) {
-                    kx[u] = load4(static_cast<const float*>(p.c.k.ptr) + page * p.c.k.sb + m.h * p.c.k.sh + (t % p.c.P) * p.c.k.st + lane * 4);
-                    vx[u] = load4(static_cast<const float*>(p.c.v.ptr) + page * p.c.v.sb + m.h * p.c.v.sh + (t % p.c.P) * p.c.v.st + lane * 4);
+                    kx[u] = load4(static_cast<const float*>(p.c.k.ptr) + page * p.c.k.sb + m.h * p.c.k.sh + slot * p.c.k.st + lane * 4);
+                    vx[u] = load4(static_cast<const float*>(p.c.v.ptr) + page * p.c.v.sb + m.h * p.c.v.sh + slot * p.c.v.st + lane * 4);
                 }
             }
             __syncthreads();                          // the preceding tile is no longer read
@@ -211,6 +211,11 @@ AttnPlan make_plan(const PagesView& c, const AttnShape& s) {
 
 }  // namespace
 
+bool paged_attention_fits(const PagesView& c, const AttnShape& s) {
+    const AttnPlan p = make_plan(c, s);
+    return (long long)p.items * (c.max_len / kTokTile + 1 + kSegCost) <= 0x7fffffffLL;
+}
+
 size_t paged_attention_bytes(const PagesView& c, const AttnShape& s) { return make_plan(c, s).bytes; }
 
 obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, TensorView q, TensorView o, float* lse, void* ws, cudaStream_t stream) {
@@ -221,7 +226,9 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
     p.q = q; p.o = o; p.lse = lse; p.nrt = plan.nrt; p.items = plan.items;
     p.one_head = c.k.sh == 0 && c.v.sh == 0 ? 1 : 0;
     p.box = 8;
-    while (p.box < kTokTile && c.P % (2 * p.box) == 0) p.box *= 2;
+    p.box_shift = 3;
+    while (p.box < kTokTile && c.P % (2 * p.box) == 0) { p.box *= 2; ++p.box_shift; }
+    p.by_G = FastDiv(s.G); p.by_nrt = FastDiv(plan.nrt);
     p.status = reinterpret_cast<unsigned int*>(w);
     p.info = reinterpret_cast<int4*>(w + plan.off_info);
     p.part_m = reinterpret_cast<float*>(w + plan.off_m); p.part_l = reinterpret_cast<float*>(w + plan.off_l);

@@ -122,13 +122,13 @@ paged_write_kernel(PagesView c, PagedWrite w, TensorView k, TensorView v, long l
         rk[i] = Row8{}; rv[i] = Row8{};
         if (f >= total) continue;
         const int unit = (int)(f / w.rows), j = (int)(f % w.rows);
-        const int b = unit / c.Hkv, h = unit % c.Hkv;
+        const int b = c.by_H.div(unit), h = unit - b * c.Hkv;
         const int n = w.new_lens ? min(max(w.new_lens[b * w.nb + h * w.nh], 0), w.rows) : w.rows;
         const int pos = c.len(b, h) - n + j;
         const int src = w.idx ? w.idx[f] : j;
         if (j >= n || pos < 0 || (unsigned)src >= (unsigned)w.src_tokens) continue;
         page[i] = c.page_of(b, h, pos);
-        slot[i] = pos % c.P; head[i] = h;
+        slot[i] = c.by_P.mod(pos); head[i] = h;
         rk[i] = load8(static_cast<const S*>(k.ptr) + b * k.sb + h * k.sh + src * k.st + lane * 8);
         rv[i] = load8(static_cast<const S*>(v.ptr) + b * v.sb + h * v.sh + src * v.st + lane * 8);
     }
@@ -153,13 +153,13 @@ paged_read_kernel(PagesView c, int n_tokens, TensorView k, TensorView v, int zer
         const long long f = f0 + i * (kBlock / kLanes);
         if (f >= total) continue;
         const int unit = (int)(f / n_tokens), t = (int)(f % n_tokens);
-        const int b = unit / c.Hkv, h = unit % c.Hkv;
+        const int b = c.by_H.div(unit), h = unit - b * c.Hkv;
         Row8 rk{}, rv{};
         if (t < c.len(b, h)) {
             const int page = c.page_of(b, h, t);
             if (page >= 0) {
-                rk = page_row<DT>(c, c.k, c.ks, page, h, t % c.P, lane * 8);
-                rv = page_row<DT>(c, c.v, c.vs, page, h, t % c.P, lane * 8);
+                rk = page_row<DT>(c, c.k, c.ks, page, h, c.by_P.mod(t), lane * 8);
+                rv = page_row<DT>(c, c.v, c.vs, page, h, c.by_P.mod(t), lane * 8);
             }
         } else if (!zero_rows) {
             continue;

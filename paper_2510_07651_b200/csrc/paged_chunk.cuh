@@ -138,10 +138,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             TileWalk<kChunkRows> walk(p, run, lane);
             uint32_t n = 0;                                         // operands issued
             while (walk.more && !fail_site) {
-                const int pg = walk.page(), h = walk.cur.m.h, t0 = walk.tile * kTokTile;
-                const bool edge = t0 + kTokTile > seen_by(p, walk.cur.m, 0);
-                walk.advance();
-                const int boxes = kTokTile / p.box, slot = (t0 + lane * p.box) % p.c.P, hh = p.one_head ? 0 : h;
+                const int pg = walk.page(), h = walk.cur.m.h, slot = walk.slot, hh = p.one_head ? 0 : h, at = lane << (p.box_shift + 7);
+                const bool edge = walk.tile * kTokTile + kTokTile > seen_by(p, walk.cur.m, 0);
                 for (int op = 0; op < 2; ++op, ++n) {
                     const CUtensorMap* map = op ? &map_v : &map_k;
                     if (E4M3) {
@@ -149,10 +147,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         if (!all_wait(L::RAWEMPTY + st, (n >> 1) ^ 1u, __LINE__)) break;
                         if (lane == 0) mbar_expect_tx(full, 16384);
                         __syncwarp();
-                        if (lane < boxes) tma_load_4d(sbase + L::kRawAt + st * 16384u + lane * p.box * 128, map, full, 0, slot, hh, pg);
-                        const int t8 = (lane & 15) * 8, ps = __shfl_sync(0xffffffffu, pg, t8 / p.box);
+                        if (lane < walk.boxes()) tma_load_4d(sbase + L::kRawAt + st * 16384u + at, map, full, 0, slot, hh, pg);
+                        const int t8 = (lane & 15) * 8, ps = __shfl_sync(0xffffffffu, pg, t8 >> p.box_shift);
                         if (lane < 16) {
-                            const uint8_t* src = (op ? p.c.vs : p.c.ks) + (ps < 0 ? 0ll : ps * p.c.ss_p + h * p.c.ss_h + (t0 + t8) % p.c.P);
+                            const uint8_t* src = (op ? p.c.vs : p.c.ks) + (ps < 0 ? 0ll : ps * p.c.ss_p + h * p.c.ss_h + walk.slot8);
                             asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(sbase + L::kScales + st * 128u + t8), "l"(src), "r"(ps < 0 ? 0 : 8) : "memory");
                         }
                         asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
@@ -161,13 +159,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         if (!all_wait(L::EMPTY + st, (n / NS) ^ 1u, __LINE__)) break;
                         if (lane == 0) mbar_expect_tx(full, kOperandBytes);
                         __syncwarp();
-                        if (lane < boxes) {
-                            const uint32_t d = sbase + L::kRing + st * kOperandBytes + lane * p.box * 128;
+                        if (lane < walk.boxes()) {
+                            const uint32_t d = sbase + L::kRing + st * kOperandBytes + at;
                             tma_load_4d(d, map, full, 0, slot, hh, pg);
                             tma_load_4d(d + kHalfBytes, map, full, 64, slot, hh, pg);
                         }
                     }
                 }
+                if (n == 2) walk.look_ahead();
+                walk.advance();
             }
             // no copy may be under way when the CTA leaves
             const uint32_t ring = E4M3 ? 2u : (uint32_t)NS;
@@ -426,7 +426,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                     for (int x = 0; x < 16; ++x) {
                                         float v = __uint_as_float(0x7fc00000u);                  // (8 bits: a scale that stands for NaN)
                                         if (!E4M3)
-                                            v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.c.v.ptr)[page * p.c.v.sb + m.h * p.c.v.sh + (t % p.c.P) * p.c.v.st + q * 16 + x]);
+                                            v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.c.v.ptr)[page * p.c.v.sb + m.h * p.c.v.sh + p.c.by_P.mod(t) * p.c.v.st + q * 16 + x]);
                                         if (j < nvis) ov[x] = __float_as_uint(fmaf(wt, v, __uint_as_float(ov[x])));
                                     }
                                     tc_st16(tO + q * 16, ov);

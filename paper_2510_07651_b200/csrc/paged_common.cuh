@@ -24,7 +24,8 @@ struct AttnParams {
     TensorView q, o;
     float* lse;                              // or nullptr
     int nrt, items;                          // row tiles per list, items in all
-    int box, one_head;                       // tokens per bulk copy; pages of one head
+    FastDiv by_G, by_nrt;
+    int box, box_shift, one_head;            // tokens per bulk copy (a power of two); pages of one head
     unsigned int* status;                    // workspace header: source line of the wait that gave up
     int4* info;                              // per CTA: the shared item that begins in it (or -1), the item's last CTA, its slot here
     float *part_m, *part_l, *part_o;         // [2 gridDim][ROWS] (x d): slots of a CTA's first and last segment
@@ -35,15 +36,15 @@ struct Item { int b, h, len, ql, r0, rows, tiles; };      // rows: rows of this 
 template <int ROWS>
 __device__ __forceinline__ Item item_of(const AttnParams& p, int it) {
     Item m;
-    const int unit = it / p.nrt;
-    m.b = unit / p.c.Hkv; m.h = unit - m.b * p.c.Hkv;
+    const int unit = p.by_nrt.div(it);
+    m.b = p.c.by_H.div(unit); m.h = unit - m.b * p.c.Hkv;
     m.len = p.c.len(m.b, m.h);
     m.ql = p.q_lens ? min(max(p.q_lens[m.b], 0), p.T) : p.T;
     m.r0 = (it - unit * p.nrt) * ROWS;
     m.rows = min(p.G * m.ql - m.r0, ROWS);
     m.tiles = 0;
     if (m.rows > 0) {                        // (one tile at least: rows that see nothing have results, too)
-        const int seen = p.causal ? min(max(m.len - m.ql + (m.r0 + m.rows - 1) / p.G + 1, 0), m.len) : m.len;
+        const int seen = p.causal ? min(max(m.len - m.ql + p.by_G.div(m.r0 + m.rows - 1) + 1, 0), m.len) : m.len;
         m.tiles = max((seen + kTokTile - 1) / kTokTile, 1);
     }
     return m;
@@ -51,7 +52,7 @@ __device__ __forceinline__ Item item_of(const AttnParams& p, int it) {
 // tokens that row r of the item's tile sees: p < the result (r beyond the tile's rows: none)
 __device__ __forceinline__ int seen_by(const AttnParams& p, const Item& m, int r) {
     if (r >= m.rows) return 0;
-    return p.causal ? min(max(m.len - m.ql + (m.r0 + r) / p.G + 1, 0), m.len) : m.len;
+    return p.causal ? min(max(m.len - m.ql + p.by_G.div(m.r0 + r) + 1, 0), m.len) : m.len;
 }
 
 // four e4m3 codes as the low and the high bytes of bf16 numbers: their bits, shifted into bf16's fields, stand for the value times 2^-120
@@ -67,8 +68,8 @@ __device__ __forceinline__ float lse_of(float ref, float total) { return (ref + 
 
 constexpr int kSegCost = 2;
 
-struct Run { long long begin, end, total, ctas; int item, off; };
-struct RunScratch { long long warp_sum[32]; Run run; };
+struct Run { int begin, end, size, longer; int item, off; };      // runs of size + 1 (the first `longer`) and of size
+struct RunScratch { int warp_sum[32]; int item, off; };
 
 // This CTA's run; all threads of the block take part.
 template <int ROWS>
@@ -76,43 +77,48 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, RunScratch* s) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, nwarps = blockDim.x >> 5;
     const int per = (p.items + blockDim.x - 1) / blockDim.x, i0 = tid * per, i1 = min(i0 + per, p.items);
     auto cost = [&](int i) { const int n = item_of<ROWS>(p, i).tiles; return n > 0 ? n + kSegCost : 0; };
-    long long mine = 0;
+    int mine = 0;
     for (int i = i0; i < i1; ++i) mine += cost(i);
-    long long scan = mine;
+    int scan = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, scan, o);
+        const int up = __shfl_up_sync(0xffffffffu, scan, o);
         if (lane >= o) scan += up;
     }
     if (lane == 31) s->warp_sum[warp] = scan;
+    if (tid == 0) { s->item = 0; s->off = 0; }
     __syncthreads();
-    long long before = scan - mine, total = 0;
+    int before = scan - mine, total = 0;
+#pragma unroll 4
     for (int w = 0; w < nwarps; ++w) {
-        if (w < warp) before += s->warp_sum[w];
-        total += s->warp_sum[w];
+        const int x = s->warp_sum[w];
+        if (w < warp) before += x;
+        total += x;
     }
     // (no empty runs between two others: the merge goes by CTA numbers)
-    const long long ctas = min((long long)gridDim.x, total);
-    const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : total, end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : total;
-    if (tid == 0) { s->run.begin = begin; s->run.end = end; s->run.total = total; s->run.ctas = ctas; s->run.item = 0; s->run.off = 0; }
-    __syncthreads();
-    if (begin >= before && begin < before + mine) {
-        long long at = before;
+    const int ctas = min((int)gridDim.x, total), cta = min((int)blockIdx.x, ctas);
+    Run run;
+    run.size = ctas ? (int)((unsigned)total / (unsigned)ctas) : 1; run.longer = total - run.size * ctas;
+    run.begin = cta * run.size + min(cta, run.longer);
+    run.end = cta < ctas ? run.begin + run.size + (cta < run.longer ? 1 : 0) : run.begin;
+    if (run.begin >= before && run.begin < before + mine) {
+        int at = before;
         for (int i = i0; i < i1; ++i) {
             const int n = cost(i);
-            if (begin < at + n) { s->run.item = i; s->run.off = (int)(begin - at); break; }
+            if (run.begin < at + n) { s->item = i; s->off = run.begin - at; break; }
             at += n;
         }
     }
     __syncthreads();
-    return s->run;
+    run.item = s->item; run.off = s->off;
+    return run;
 }
 
 // Walks the segments of a run; every role of a CTA has its own copy.
 template <int ROWS>
 struct Segments {
     const AttnParams& p;
-    long long at, end;                       // where the next item begins; the run's end
+    int at, end;                             // where the next item begins; the run's end
     int next_item, off;                      // off: what of the next item's cost lies before the run
     Item m;                                  // the segment: tiles [ta, tb) of item `item`
     int item, ta, tb;
@@ -124,7 +130,7 @@ struct Segments {
             m = item_of<ROWS>(p, next_item++);
             if (m.tiles == 0) continue;
             ta = max(off - kSegCost, 0);
-            tb = (int)max(min(end - at - kSegCost, (long long)m.tiles), 0ll);
+            tb = max(min(end - at - kSegCost, m.tiles), 0);
             at += m.tiles + kSegCost;
             off = 0;
             if (ta < tb) { item = next_item - 1; return true; }
@@ -137,7 +143,9 @@ struct Segments {
     // of the current segment, for the merge
     __device__ __forceinline__ int4 shared_item(const Run& r) const {
         if (ta != 0 || tb == m.tiles) return make_int4(-1, 0, 0, 0);
-        return make_int4(item, (int)((at * r.ctas + r.total - 1) / r.total) - 1, first ? 0 : 1, 0);        // at - 1: the item's last tile
+        const int last = at - 1, split = r.longer * (r.size + 1);                  // the item's last tile
+        const int cta = last < split ? last / (r.size + 1) : r.longer + (last - split) / r.size;
+        return make_int4(item, cta, first ? 0 : 1, 0);
     }
 };
 
@@ -150,20 +158,31 @@ struct TileWalk {
     const AttnParams& p;
     Segments<ROWS> cur, nxt;
     bool more, more_next;
-    int lane, boxes, tile, pages, pages_next;
+    int lane, tile, pages, pages_next;
+    int slot, slot8, step;                   // places in their pages of the lane's box and of the lane's eight tokens (of 16 lanes); 128 mod P
     __device__ __forceinline__ TileWalk(const AttnParams& p_, const Run& r, int lane_) : p(p_), cur(p_, r), nxt(p_, r), lane(lane_) {
-        boxes = kTokTile / p.box;
+        step = p.c.by_P.mod(kTokTile);
         more = cur.next();
-        nxt.next(); more_next = nxt.next();
-        tile = cur.ta;
         pages = pages_next = -1;
-        if (more) { pages = asked(cur.m, window(tile)); ahead(); }
+        more_next = false;
+        if (more) { begin(); pages = asked(cur.m, window(tile)); }
     }
-    __device__ __forceinline__ int window(int t) const { return t * boxes >> 5; }
+    // what need not be known before the first tile's copies are on their way
+    __device__ __forceinline__ void look_ahead() {
+        if (!more) return;
+        nxt.copy(cur); more_next = nxt.next();
+        ahead();
+    }
+    __device__ __forceinline__ int boxes() const { return kTokTile >> p.box_shift; }
+    __device__ __forceinline__ int window(int t) const { return t >> (p.box_shift - 2); }                  // 32 boxes = 2^(shift + 5) tokens
+    __device__ __forceinline__ void begin() {
+        tile = cur.ta;
+        slot = p.c.by_P.mod(tile * kTokTile + (lane << p.box_shift)); slot8 = p.c.by_P.mod(tile * kTokTile + (lane & 15) * 8);
+    }
     __device__ __forceinline__ int asked(const Item& m, int win) const {
-        const int t = (win * 32 + lane) * p.box;
+        const int t = (win * 32 + lane) << p.box_shift;
         int v = -1;
-        if (t < m.len) v = p.c.table[m.b * p.c.tb + m.h * p.c.th + t / p.c.P];
+        if (t < m.len) v = p.c.table[m.b * p.c.tb + m.h * p.c.th + p.c.by_P.div(t)];
         return v;
     }
     __device__ __forceinline__ void ahead() {
@@ -172,18 +191,21 @@ struct TileWalk {
     }
     // page of the lane's box of the current tile; -1 for rows of zeros (behind the list, or a page that is not there)
     __device__ __forceinline__ int page() const {
-        const int v = __shfl_sync(0xffffffffu, pages, (tile * boxes + lane) & 31);
-        return lane < boxes && (unsigned)v < (unsigned)p.c.n_pages ? v : -1;
+        const int v = __shfl_sync(0xffffffffu, pages, (tile * boxes() + lane) & 31);
+        return lane < boxes() && (unsigned)v < (unsigned)p.c.n_pages ? v : -1;
     }
     __device__ __forceinline__ void advance() {
         if (++tile < cur.tb) {
+            slot += step; slot8 += step;
+            if (slot >= p.c.P) slot -= p.c.P;
+            if (slot8 >= p.c.P) slot8 -= p.c.P;
             if (window(tile) != window(tile - 1)) { pages = pages_next; ahead(); }
             return;
         }
         more = more_next;
         if (!more) return;
         cur.copy(nxt);
-        tile = cur.ta;
+        begin();
         pages = pages_next;
         more_next = nxt.next();
         ahead();
@@ -193,7 +215,7 @@ struct TileWalk {
 // where the row (i G + g) of an item's list stands in q, o and lse
 __device__ __forceinline__ void row_place(const AttnParams& p, const Item& m, int r, int& head, int& i) {
     const int row = m.r0 + r;
-    i = row / p.G;
+    i = p.by_G.div(row);
     head = m.h * p.G + (row - i * p.G);
 }
 

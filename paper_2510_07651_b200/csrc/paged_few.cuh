@@ -72,24 +72,24 @@ template <int N> __device__ __forceinline__ bool consumers_or(bool x) {
 // 2^(s - 67): a row's scale with the 2^60 that is due beside it
 __device__ __forceinline__ float scale_60(uint32_t s) { return __uint_as_float(s > 186u ? 0x7fc00000u : (s + 60u) << 23); }
 
-// Copies the tile's pages (and scales) into a stage; all lanes of a warp.  `page`: of the lane's box, -1 for rows of zeros.
-template <typename L, bool E4M3>
-__device__ __forceinline__ void few_issue(const AttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, uint32_t stage, uint32_t scales, uint32_t bar,
-                                          int lane, int page, int h, int t0) {
+// Copies the pages (and scales) of the walk's tile into a stage; all lanes of a warp.
+template <typename L, bool E4M3, typename W>
+__device__ __forceinline__ void few_issue(const W& walk, const CUtensorMap* mk, const CUtensorMap* mv, uint32_t stage, uint32_t scales, uint32_t bar) {
+    const AttnParams& p = walk.p;
+    const int lane = walk.lane, page = walk.page(), h = walk.cur.m.h;
     if (lane == 0) mbar_expect_tx(bar, L::kStage);
     __syncwarp();
-    const int n = kTokTile / p.box, slot = (t0 + lane * p.box) % p.c.P, hh = p.one_head ? 0 : h;
-    if (lane < n) {
-        const uint32_t d = stage + lane * p.box * 128;
+    if (lane < walk.boxes()) {
+        const uint32_t d = stage + (lane << (p.box_shift + 7));
+        const int hh = p.one_head ? 0 : h, slot = walk.slot;
         tma_load_4d(d, mk, bar, 0, slot, hh, page);
         if (!E4M3) tma_load_4d(d + kHalfBytes, mk, bar, 64, slot, hh, page);
         tma_load_4d(d + L::kOperand, mv, bar, 0, slot, hh, page);
         if (!E4M3) tma_load_4d(d + L::kOperand + kHalfBytes, mv, bar, 64, slot, hh, page);
     }
     if (E4M3) {                              // 8 scale bytes per lane: lanes 0-15 K, 16-31 V
-        const int t8 = (lane & 15) * 8, pg = __shfl_sync(0xffffffffu, page, t8 / p.box);
-        const uint8_t* base = lane < 16 ? p.c.ks : p.c.vs;
-        const uint8_t* src = base + (pg < 0 ? 0ll : pg * p.c.ss_p + h * p.c.ss_h + (t0 + t8) % p.c.P);
+        const int t8 = (lane & 15) * 8, pg = __shfl_sync(0xffffffffu, page, t8 >> p.box_shift);
+        const uint8_t* src = (lane < 16 ? p.c.ks : p.c.vs) + (pg < 0 ? 0ll : pg * p.c.ss_p + h * p.c.ss_h + walk.slot8);
         asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(scales + (lane >> 4) * 128 + t8), "l"(src), "r"(pg < 0 ? 0 : 8) : "memory");
         asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
     }
@@ -126,10 +126,10 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         int n = 0, st = 0, fb = 0;                                  // tiles issued; stage and barrier of the next
         uint32_t phase = 1;
         while (walk.more) {
-            const int pg = walk.page(), h = walk.cur.m.h, t0 = walk.tile * kTokTile;
-            walk.advance();
             if (!__all_sync(0xffffffffu, mbar_wait(empty(st), phase))) { fail_site = __LINE__; break; }
-            few_issue<L, E4M3>(p, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(fb), lane, pg, h, t0);
+            few_issue<L, E4M3>(walk, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(fb));
+            if (n == 0) walk.look_ahead();
+            walk.advance();
             ++n;
             if (++fb == L::kFull) fb = 0;
             if (++st == L::kStages) { st = 0; phase ^= 1u; }
@@ -168,7 +168,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
 #pragma unroll
                 for (int j = 0; j < 8; ++j) { o[nt][j][0] = 0.f; o[nt][j][1] = 0.f; o[nt][j][2] = 0.f; o[nt][j][3] = 0.f; }
             }
-            const int first_masked = p.causal ? min(max(m.len - m.ql + m.r0 / p.G + 1, 0), m.len) : m.len;   // tokens that not every row sees begin here
+            const int first_masked = p.causal ? min(max(m.len - m.ql + p.by_G.div(m.r0) + 1, 0), m.len) : m.len;   // tokens that not every row sees begin here
 
             for (int tile = seg.ta; tile < seg.tb; ++tile) {
                 const bool mine = L::kGroups == 1 || turn == group;
