@@ -190,8 +190,9 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
 bool make_map(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
               uint32_t box_rows);
 // the pages of a paged cache (bf16 or e4m3): dimensions channel, token of the page, head, page; box of 128 bytes of `box` tokens,
-// 128-byte swizzle.  A negative page number reads as zeros.
-bool make_page_map(CUtensorMap* map, const PagesView& c, const TensorView& t, int box);
+// 128-byte swizzle.  whole_rows: 16-bit rows in one copy, as [half of the channels][token][128 bytes], with a dimension for the halves behind
+// that of the tokens.  A negative page number reads as zeros.
+bool make_page_map(CUtensorMap* map, const PagesView& c, const TensorView& t, int box, bool whole_rows);
 
 // ---- programmatic dependent launch ------------------------------------------------------------
 // Every kernel of the library is launched with programmatic stream serialization: its CTAs may

@@ -16,51 +16,47 @@ namespace {
 
 // ---- merge ------------------------------------------------------------------------------------------
 // One warp per row of an item that was shared: o = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the CTAs' slots, in
-// their order.  A block takes `kMergeRows` rows of the item that begins in CTA blockIdx.x / (blocks per item).
-template <int ROWS> struct MergeShape { static constexpr int kRows = ROWS < 32 ? 8 : 32, kBlocks = ROWS / kRows; };
-
+// their order.  A block takes eight rows of the item that begins in CTA blockIdx.x / (blocks per item).
 template <typename OT, int ROWS>
 __global__ void __launch_bounds__(256)
 paged_merge_kernel(const __grid_constant__ AttnParams p) {
-    using S = MergeShape<ROWS>;
+    constexpr int kBlocks = ROWS / 8;
     pdl_wait();
-    const int cta = blockIdx.x / S::kBlocks, lane = threadIdx.x & 31;
+    const int cta = blockIdx.x / kBlocks, lane = threadIdx.x & 31;
     const int4 f = p.info[cta];
     if (f.x < 0) return;
     const Item m = item_of<ROWS>(p, f.x);
     const int n = f.y - cta + 1;
-    for (int rr = threadIdx.x >> 5; rr < S::kRows; rr += 8) {
-        const int r = (blockIdx.x % S::kBlocks) * S::kRows + rr;
-        if (r >= m.rows) return;
-        auto at = [&](int s) { return (2 * (size_t)(cta + s) + (s == 0 ? f.z : 0)) * ROWS + r; };
-        float top = -INFINITY;
-        for (int s = lane; s < n; s += 32) top = fmaxf(top, p.part_m[at(s)]);
-        top = warp_max(top);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float total = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s0 = 0; s0 < n; s0 += 32) {
-            const int s = s0 + lane, cnt = min(32, n - s0);
-            const float w = s < n ? exp2f(p.part_m[at(s)] - ref) : 0.f;
-            if (s < n) total = fmaf(w, p.part_l[at(s)], total);
-    #pragma unroll 4
-            for (int j = 0; j < cnt; ++j) {
-                const float wj = __shfl_sync(0xffffffffu, w, j);
-                const float4 o = *reinterpret_cast<const float4*>(p.part_o + at(s0 + j) * kD + lane * 4);
-                if (wj == 0.f) continue;         // nothing was seen there (or nothing that counts)
-                acc.x = fmaf(wj, o.x, acc.x); acc.y = fmaf(wj, o.y, acc.y); acc.z = fmaf(wj, o.z, acc.z); acc.w = fmaf(wj, o.w, acc.w);
-            }
+    const int r = (blockIdx.x % kBlocks) * 8 + (threadIdx.x >> 5);
+    if (r >= m.rows) return;
+    auto at = [&](int s) { return (2 * (size_t)(cta + s) + (s == 0 ? f.z : 0)) * ROWS + r; };
+    float top = -INFINITY;
+    for (int s = lane; s < n; s += 32) top = fmaxf(top, p.part_m[at(s)]);
+    top = warp_max(top);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < n; s0 += 32) {
+        const int s = s0 + lane, cnt = min(32, n - s0);
+        const float w = s < n ? exp2f(p.part_m[at(s)] - ref) : 0.f;
+        if (s < n) total = fmaf(w, p.part_l[at(s)], total);
+#pragma unroll 8
+        for (int j = 0; j < cnt; ++j) {
+            const float wj = __shfl_sync(0xffffffffu, w, j);
+            const float4 o = *reinterpret_cast<const float4*>(p.part_o + at(s0 + j) * kD + lane * 4);
+            if (wj == 0.f) continue;         // nothing was seen there (or nothing that counts)
+            acc.x = fmaf(wj, o.x, acc.x); acc.y = fmaf(wj, o.y, acc.y); acc.z = fmaf(wj, o.z, acc.z); acc.w = fmaf(wj, o.w, acc.w);
         }
-        total = warp_sum(total);
-        const float inv = total != 0.f ? 1.f / total : 0.f;
-        int head, i;
-        row_place(p, m, r, head, i);
-        OT* dst = static_cast<OT*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + i * p.o.st + lane * 4;
-        if constexpr (sizeof(OT) == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-        else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (p.lse && lane == 0)
-            p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + i] = lse_of(ref, total);
     }
+    total = warp_sum(total);
+    const float inv = total != 0.f ? 1.f / total : 0.f;
+    int head, i;
+    row_place(p, m, r, head, i);
+    OT* dst = static_cast<OT*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + i * p.o.st + lane * 4;
+    if constexpr (sizeof(OT) == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    if (p.lse && lane == 0)
+        p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + i] = lse_of(ref, total);
 }
 
 // ---- fp32 on CUDA cores ---------------------------------------------------------------------------------
@@ -240,7 +236,8 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
         e = launch_pdl(paged_f32_kernel, dim3(plan.grid), dim3(kF32Threads), kF32Smem, stream, 1, p);
     } else {
         CUtensorMap mk, mv;
-        if (!make_page_map(&mk, c, c.k, p.box) || !make_page_map(&mv, c, c.v, p.box)) return OBC_ERR_CUDA;
+        const bool whole_rows = plan.rows != kChunkRows;
+        if (!make_page_map(&mk, c, c.k, p.box, whole_rows) || !make_page_map(&mv, c, c.v, p.box, whole_rows)) return OBC_ERR_CUDA;
         auto few = [&](auto kernel, auto layout) {
             using L = decltype(layout);
             const cudaError_t a = allow_smem(kernel, L::kSmem);
@@ -270,10 +267,10 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
         ProfScope prof("paged_attention_merge", stream);
         return launch_pdl(kernel, dim3((unsigned)(plan.grid * blocks)), dim3(256), 0, stream, 1, p);
     };
-    OBC_CUDA_TRY(c.dtype == OBC_F32 ? merge(paged_merge_kernel<float, kF32Rows>, MergeShape<kF32Rows>::kBlocks)
-                 : plan.rows == 8   ? merge(paged_merge_kernel<__nv_bfloat16, 8>, MergeShape<8>::kBlocks)
-                 : plan.rows == 16  ? merge(paged_merge_kernel<__nv_bfloat16, 16>, MergeShape<16>::kBlocks)
-                                    : merge(paged_merge_kernel<__nv_bfloat16, kChunkRows>, MergeShape<kChunkRows>::kBlocks));
+    OBC_CUDA_TRY(c.dtype == OBC_F32 ? merge(paged_merge_kernel<float, kF32Rows>, kF32Rows / 8)
+                 : plan.rows == 8   ? merge(paged_merge_kernel<__nv_bfloat16, 8>, 8 / 8)
+                 : plan.rows == 16  ? merge(paged_merge_kernel<__nv_bfloat16, 16>, 16 / 8)
+                                    : merge(paged_merge_kernel<__nv_bfloat16, kChunkRows>, kChunkRows / 8));
     return OBC_OK;
 }
 

@@ -21,7 +21,7 @@ namespace obc {
 namespace {
 
 template <int NT, bool E4M3> struct FewLayout {
-    static constexpr int kRows = 8 * NT, kGroups = NT == 1 ? 2 : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 32;
+    static constexpr int kRows = 8 * NT, kGroups = NT == 1 ? 2 : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 64;
     static constexpr uint32_t kOperand = kTokTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
     static constexpr int kStages = E4M3 ? 5 : 3, kFull = kStages * kGroups;
     static constexpr int kPitch = kD + 4;                                                  // floats per row of O in the merge buffer
@@ -72,27 +72,32 @@ template <int N> __device__ __forceinline__ bool consumers_or(bool x) {
 // 2^(s - 67): a row's scale with the 2^60 that is due beside it
 __device__ __forceinline__ float scale_60(uint32_t s) { return __uint_as_float(s > 186u ? 0x7fc00000u : (s + 60u) << 23); }
 
-// Copies the pages (and scales) of the walk's tile into a stage; all lanes of a warp.
+// Copies the pages (and scales) of the walk's tile into a stage, K or V (`scale` and `stage` are that operand's); all lanes of a warp.  A copy takes a
+// warp some hundred cycles to issue, one lane after the other, which is what two warps and the map that takes both halves of the rows at
+// once are for: a tile in pages of 16 tokens is 8 copies per warp.
 template <typename L, bool E4M3, typename W>
-__device__ __forceinline__ void few_issue(const W& walk, const CUtensorMap* mk, const CUtensorMap* mv, uint32_t stage, uint32_t scales, uint32_t bar) {
+__device__ __forceinline__ void few_issue(const W& walk, const CUtensorMap* map, const uint8_t* scale, uint32_t stage, uint32_t scales, uint32_t bar) {
     const AttnParams& p = walk.p;
     const int lane = walk.lane, page = walk.page(), h = walk.cur.m.h;
-    if (lane == 0) mbar_expect_tx(bar, L::kStage);
+    if (lane == 0) mbar_expect_tx(bar, L::kOperand);
     __syncwarp();
     if (lane < walk.boxes()) {
-        const uint32_t d = stage + (lane << (p.box_shift + 7));
+        const uint32_t d = stage + (lane << (p.box_shift + (E4M3 ? 7 : 8)));
         const int hh = p.one_head ? 0 : h, slot = walk.slot;
-        tma_load_4d(d, mk, bar, 0, slot, hh, page);
-        if (!E4M3) tma_load_4d(d + kHalfBytes, mk, bar, 64, slot, hh, page);
-        tma_load_4d(d + L::kOperand, mv, bar, 0, slot, hh, page);
-        if (!E4M3) tma_load_4d(d + L::kOperand + kHalfBytes, mv, bar, 64, slot, hh, page);
+        if (E4M3) tma_load_4d(d, map, bar, 0, slot, hh, page);
+        else tma_load_5d(d, map, bar, 0, slot, 0, hh, page);
     }
-    if (E4M3) {                              // 8 scale bytes per lane: lanes 0-15 K, 16-31 V
+    if (E4M3) {                              // 8 scale bytes per lane of the first 16
         const int t8 = (lane & 15) * 8, pg = __shfl_sync(0xffffffffu, page, t8 >> p.box_shift);
-        const uint8_t* src = (lane < 16 ? p.c.ks : p.c.vs) + (pg < 0 ? 0ll : pg * p.c.ss_p + h * p.c.ss_h + walk.slot8);
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(scales + (lane >> 4) * 128 + t8), "l"(src), "r"(pg < 0 ? 0 : 8) : "memory");
+        const uint8_t* src = scale + (pg < 0 ? 0ll : pg * p.c.ss_p + h * p.c.ss_h + walk.slot8);
+        if (lane < 16) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(scales + t8), "l"(src), "r"(pg < 0 ? 0 : 8) : "memory");
         asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(bar) : "memory");
     }
+}
+// 16-byte piece `piece` of row `row` of a staged tile of 16-bit values: [box][half of the channels][row of the box][128 bytes], swizzled
+__device__ __forceinline__ uint32_t few_piece(int box_shift, int row, int piece) {
+    const int in_box = row & ((1 << box_shift) - 1);
+    return (uint32_t)((row >> box_shift) << (box_shift + 8)) + (uint32_t)((piece >> 3) << (box_shift + 7)) + in_box * 128 + (((piece & 7) ^ (row & 7)) << 4);
 }
 
 template <int NT, bool E4M3>
@@ -111,7 +116,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     auto empty = [&](int i) { return sbase + L::kBars + 8u * (uint32_t)(L::kFull + i); };
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
-        for (int i = 0; i < L::kFull; ++i) mbar_init(full(i), E4M3 ? 33 : 1);
+        for (int i = 0; i < L::kFull; ++i) mbar_init(full(i), E4M3 ? 66 : 2);
         for (int i = 0; i < L::kStages; ++i) mbar_init(empty(i), 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -120,14 +125,15 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     const Run run = find_run<ROWS>(p, &scratch);                    // (its barriers also publish the mbarriers)
     int fail_site = 0;
 
-    if (warp == L::kWarps) {
-        // ===================================== producer =====================================
+    if (warp >= L::kWarps) {
+        // ============================ producers: a warp for K, one for V =====================
+        const bool is_v = warp > L::kWarps;
         TileWalk<ROWS> walk(p, run, lane);
         int n = 0, st = 0, fb = 0;                                  // tiles issued; stage and barrier of the next
         uint32_t phase = 1;
         while (walk.more) {
             if (!__all_sync(0xffffffffu, mbar_wait(empty(st), phase))) { fail_site = __LINE__; break; }
-            few_issue<L, E4M3>(walk, &map_k, &map_v, sbase + st * L::kStage, sbase + L::kScales + st * 256, full(fb));
+            few_issue<L, E4M3>(walk, is_v ? &map_v : &map_k, is_v ? p.c.vs : p.c.ks, sbase + st * L::kStage + (is_v ? L::kOperand : 0u), sbase + L::kScales + st * 256 + (is_v ? 128 : 0), full(fb));
             if (n == 0) walk.look_ahead();
             walk.advance();
             ++n;
@@ -209,7 +215,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         for (int ks = 0; ks < 8; ++ks) {
                             const int piece = 2 * ks + a_pc;
                             uint32_t a[4];
-                            ldsm_x4(a, sk + (piece >> 3) * kHalfBytes + a_row * 128 + (((piece & 7) ^ (a_row & 7)) << 4));
+                            ldsm_x4(a, sk + few_piece(p.box_shift, a_row, piece));
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) mma_bf16(ks & 1 ? s2[nt] : s[nt], a, qf[nt][ks][0], qf[nt][ks][1]);
                         }
@@ -266,7 +272,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         // is not finite must reach the queries that see it alone
                         bool odd = false;
                         const int row = tok0 + (lane >> 1), t = t0 + (lane >> 1);
-                        uint4* at = reinterpret_cast<uint4*>(sv + (lane & 1) * kHalfBytes + row * 128);
+                        uint4* at = reinterpret_cast<uint4*>(sv + (few_piece(p.box_shift, row, (lane & 1) * 8) & ~127u));      // the row's half
                         if (t >= m.len) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j) at[j] = make_uint4(0u, 0u, 0u, 0u);
@@ -291,13 +297,13 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                                     if (t0 + tk >= seen[nt][j]) continue;
 #pragma unroll
                                     for (int x = 0; x < 16; ++x) {  // channels 8 x + g
-                                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(sv + (x >> 3) * kHalfBytes + rw * 128 + (((x & 7) ^ (rw & 7)) << 4) + g * 2);
+                                        const __nv_bfloat16 v = *reinterpret_cast<const __nv_bfloat16*>(sv + few_piece(p.box_shift, rw, x) + g * 2);
                                         o[nt][x >> 1][(x & 1) * 2 + j] += w[j] * __bfloat162float(v);
                                     }
                                 }
                             }
                             __syncwarp();
-                            if (lane < 16) *reinterpret_cast<uint4*>(sv + (lane >> 3) * kHalfBytes + rw * 128 + ((lane & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                            if (lane < 16) *reinterpret_cast<uint4*>(sv + few_piece(p.box_shift, rw, lane)) = make_uint4(0u, 0u, 0u, 0u);
                             __syncwarp();
                         }
                     }
@@ -322,7 +328,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         for (int j = 0; j < 8; ++j) {
                             const int piece = 2 * j + v_pc;
                             uint32_t a[4];
-                            ldsm_x4_trans(a, sv + (piece >> 3) * kHalfBytes + v_row * 128 + (((piece & 7) ^ (v_row & 7)) << 4));
+                            ldsm_x4_trans(a, sv + few_piece(p.box_shift, v_row, piece));
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_bf16(o[nt][j], a, ph[nt][0], ph[nt][1]);

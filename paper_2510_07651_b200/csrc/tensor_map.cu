@@ -61,17 +61,21 @@ bool make_map(CUtensorMap* map, const void* base, int rank, const uint64_t* dims
 }
 
 // (made anew for every call: a pool's map is not worth a slot of the cache above)
-bool make_page_map(CUtensorMap* map, const PagesView& c, const TensorView& t, int box) {
+bool make_page_map(CUtensorMap* map, const PagesView& c, const TensorView& t, int box, bool whole_rows) {
     PFN_cuTensorMapEncodeTiled enc = get_encode();
     if (!enc) return false;
     const bool e4m3 = c.dtype == OBC_E4M3;
-    const cuuint64_t es = e4m3 ? 1 : 2;
-    const cuuint64_t row = (cuuint64_t)t.st * es;
+    const cuuint64_t es = e4m3 ? 1 : 2, row = (cuuint64_t)t.st * es;
     // (a stride of 0, which the encoding refuses, belongs to a dimension of extent 1)
-    const cuuint64_t dims[4] = {(cuuint64_t)kD, (cuuint64_t)c.P, (cuuint64_t)(t.sh ? c.Hkv : 1), (cuuint64_t)(t.sb ? c.n_pages : 1)};
-    const cuuint64_t strides[3] = {row, t.sh ? (cuuint64_t)t.sh * es : row, t.sb ? (cuuint64_t)t.sb * es : row};
-    const cuuint32_t boxes[4] = {e4m3 ? 128u : 64u, (cuuint32_t)box, 1, 1}, ones[4] = {1, 1, 1, 1};
-    return enc(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(t.ptr), dims, strides, boxes, ones,
+    cuuint64_t dims[5] = {e4m3 ? 128u : 64u, (cuuint64_t)c.P}, strides[4] = {row};
+    cuuint32_t boxes[5] = {e4m3 ? 128u : 64u, (cuuint32_t)box, 1, 1, 1};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+    int n = 2;
+    if (whole_rows && !e4m3) { dims[n] = 2; strides[n - 1] = 128; boxes[n++] = 2; }
+    else dims[0] = kD;
+    dims[n] = (cuuint64_t)(t.sh ? c.Hkv : 1); strides[n - 1] = t.sh ? (cuuint64_t)t.sh * es : row; ++n;
+    dims[n] = (cuuint64_t)(t.sb ? c.n_pages : 1); strides[n - 1] = t.sb ? (cuuint64_t)t.sb * es : row; ++n;
+    return enc(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)n, const_cast<void*>(t.ptr), dims, strides, boxes, ones,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
