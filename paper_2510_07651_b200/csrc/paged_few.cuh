@@ -8,10 +8,13 @@
 // more than its own rounding (the MMAs are nowhere near their limit here).  What sets the pace is the chain of dependent steps of a warp
 // per tile, hence two groups of eight warps on alternate tiles where the registers allow it (8 rows).
 //
-// e4m3 rows are expanded in registers: the code's bits, shifted into bf16's fields, are the value times 2^-120 (subnormals included).  The
-// channels of a 16-channel step are taken in the order in which ldmatrix hands out their bytes (q is loaded in the same order), and the
-// rows of an O^T tile are eight even and eight odd channels.  2^60 goes into q; the scale of a K row, 2^60 and the rest of 2^120 into
-// its logit, that of a V row and 2^60 into its P, and the last 2^60 into the result.
+// e4m3 rows become fp16 in registers, which holds every code exactly (one conversion for two codes; to bf16 it took seven instructions for
+// four and, since P then needs two parts, twice the MMAs: 256 lists of 4096 tokens 80 us against 62).  The channels of a 16-channel step are
+// taken in the order in which ldmatrix hands out their bytes (q is loaded in the same order), and the rows of an O^T tile are eight even and
+// eight odd channels.  q is scaled by a power of two per row, so that its largest value is near 2^14 (what falls below fp16's range is less
+// than 2^-38 of it).  The scale of a K row goes into its logit, that of a V row into its P, relative to a reference exponent that O carries: P is
+// fp16 then, off by at most 2^-11 of itself.  Where the V rows of 16 tokens lie further apart than fp16's range allows they are taken by
+// classes of exponents.
 #pragma once
 #include "paged_common.cuh"
 #include "tc_ptx.cuh"
@@ -31,29 +34,52 @@ template <int NT, bool E4M3> struct FewLayout {
     static constexpr uint32_t kSmem = kBars + (kFull + kStages) * 8u + 1024;               // + alignment slack
 };
 
-// (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3), of four codes as bf16 pairs, each value times 2^-120
+// four e4m3 codes as fp16 pairs: (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3)
 __device__ __forceinline__ void expand_adjacent(uint32_t x, uint32_t& p01, uint32_t& p23) {
-    uint32_t lo, hi;
-    expand(x, lo, hi);
-    p01 = __byte_perm(lo, hi, 0x5140); p23 = __byte_perm(lo, hi, 0x7362);
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(p01), "=r"(p23) : "r"(x));
 }
-__device__ __forceinline__ void expand_alternate(uint32_t x, uint32_t& p02, uint32_t& p13) {
-    uint32_t lo, hi;
-    expand(x, lo, hi);
-    p02 = __byte_perm(lo, hi, 0x6240); p13 = __byte_perm(lo, hi, 0x7351);
+__device__ __forceinline__ void expand_alternate(uint32_t x, uint32_t& p02, uint32_t& p13) { expand_adjacent(__byte_perm(x, 0u, 0x3120), p02, p13); }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
-// B operand of step ks from one row of q: channels 16 ks + 2 c, + 1 and + 8, + 9; e4m3: 16 ks + 4 c, .. + 3, times 2^60.  nullptr: zeros.
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 2^e for whole e (0 and infinity beyond fp32's exponents)
+__device__ __forceinline__ float pow2i(int e) { return e < -126 ? 0.f : e > 127 ? INFINITY : __uint_as_float((uint32_t)(e + 127) << 23); }
+// a row's scale from its byte
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s == 0u ? 0x00400000u : s << 23); }
+
+// B operands of all steps from one row of q (nullptr: zeros): channels 16 ks + 2 c, + 1 and + 8, + 9.  e4m3: 16 ks + 4 c, .. + 3 as fp16 times a
+// power of two; the result is what undoes it.  The four lanes of a row call together.
 template <bool E4M3>
-__device__ __forceinline__ void q_fragment(uint32_t (&b)[2], const __nv_bfloat16* src, int ks, int c) {
-    if (E4M3) {
-        const uint2 u = src ? *reinterpret_cast<const uint2*>(src + ks * 16 + c * 4) : make_uint2(0u, 0u);
-        const __nv_bfloat162 up = __floats2bfloat162_rn(0x1p60f, 0x1p60f);
-        const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u.x), up), y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u.y), up);
-        b[0] = *reinterpret_cast<const uint32_t*>(&x); b[1] = *reinterpret_cast<const uint32_t*>(&y);
-    } else {
+__device__ __forceinline__ float q_fragments(uint32_t (&b)[8][2], const __nv_bfloat16* src, int c) {
+    if (!E4M3) {
         const uint32_t* u = reinterpret_cast<const uint32_t*>(src);
-        b[0] = u ? u[ks * 8 + c] : 0u; b[1] = u ? u[ks * 8 + 4 + c] : 0u;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) { b[ks][0] = u ? u[ks * 8 + c] : 0u; b[ks][1] = u ? u[ks * 8 + 4 + c] : 0u; }
+        return 1.f;
     }
+    uint32_t top = 0;                        // largest |q|, as bf16 bits
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+        const uint2 u = src ? *reinterpret_cast<const uint2*>(src + ks * 16 + c * 4) : make_uint2(0u, 0u);
+        b[ks][0] = u.x; b[ks][1] = u.y;
+        top = max(top, max(max(u.x & 0x7fffu, u.x >> 16 & 0x7fffu), max(u.y & 0x7fffu, u.y >> 16 & 0x7fffu)));
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int e = (int)(top >> 7);           // biased exponent; 0: zeros or subnormals, 255: infinity or NaN (the row's result is NaN either way)
+    const int up = e == 255 ? 0 : min(141 - e, 127);
+    const float f = pow2i(up);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) b[ks][j] = pack_f16x2(__uint_as_float(b[ks][j] << 16) * f, __uint_as_float(b[ks][j] & 0xffff0000u) * f);
+    return pow2i(-up);
 }
 // an 8x8 tile of 16-bit values turned: the lane's pair (row lane / 4, columns 2 (lane % 4), + 1) becomes that of the transpose
 __device__ __forceinline__ uint32_t turned(uint32_t x) {
@@ -69,9 +95,6 @@ template <int N> __device__ __forceinline__ bool consumers_or(bool x) {
                  : "=r"(r) : "r"((uint32_t)x), "n"(N) : "memory");
     return r != 0;
 }
-// 2^(s - 67): a row's scale with the 2^60 that is due beside it
-__device__ __forceinline__ float scale_60(uint32_t s) { return __uint_as_float(s > 186u ? 0x7fc00000u : (s + 60u) << 23); }
-
 // Copies the pages (and scales) of the walk's tile into a stage, K or V (`scale` and `stage` are that operand's); all lanes of a warp.  A copy takes a
 // warp some hundred cycles to issue, one lane after the other, which is what two warps and the map that takes both halves of the rows at
 // once are for: a tile in pages of 16 tokens is 8 copies per warp.
@@ -157,7 +180,8 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             info = seg.shared_item(run);
             uint32_t qf[NT][8][2];
             int seen[NT][2];                                        // of rows 2 c, 2 c + 1
-            float mx[NT][2], l[NT][2];
+            float mx[NT][2], l[NT][2], sl2[NT][2];
+            int e_ref = -1;                                         // biased exponent that the warp's O is relative to (e4m3); -1: none yet
             float o[NT][8][4];                                      // O^T: channel tile; (row g, columns 2 c, 2 c + 1), (row g + 8, ..)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -167,8 +191,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                     row_place(p, m, nt * 8 + g, head, i);
                     src = static_cast<const __nv_bfloat16*>(p.q.ptr) + m.b * p.q.sb + head * p.q.sh + i * p.q.st;
                 }
+                const float down = q_fragments<E4M3>(qf[nt], src, c);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) q_fragment<E4M3>(qf[nt][ks], src, ks, c);
+                for (int j = 0; j < 2; ++j) sl2[nt][j] = E4M3 ? p.sl2 * __shfl_sync(0xffffffffu, down, 4 * (2 * c + j)) : p.sl2;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) { seen[nt][j] = seen_by(p, m, nt * 8 + 2 * c + j); mx[nt][j] = -INFINITY; l[nt][j] = 0.f; }
 #pragma unroll
@@ -206,8 +231,8 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             expand_adjacent(r[2], b[0], b[2]); expand_adjacent(r[3], b[1], b[3]);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
-                                mma_bf16(s[nt], a, qf[nt][pc][0], qf[nt][pc][1]);
-                                mma_bf16(s2[nt], b, qf[nt][pc + 1][0], qf[nt][pc + 1][1]);
+                                mma_f16(s[nt], a, qf[nt][pc][0], qf[nt][pc][1]);
+                                mma_f16(s2[nt], b, qf[nt][pc + 1][0], qf[nt][pc + 1][1]);
                             }
                         }
                     } else {
@@ -220,11 +245,28 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             for (int nt = 0; nt < NT; ++nt) mma_bf16(ks & 1 ? s2[nt] : s[nt], a, qf[nt][ks][0], qf[nt][ks][1]);
                         }
                     }
-                    float fk[2] = {p.sl2, p.sl2}, fv[2] = {1.f, 1.f};            // factors of the lane's tokens g and g + 8
+                    float fk[2] = {1.f, 1.f}, fv[2] = {1.f, 1.f};                // factors of the lane's tokens g and g + 8
+                    int ev[2] = {0, 0};
+                    bool classes = false;
                     if (E4M3) {
                         const uint8_t* sc = smem + L::kScales + s_at * 256 + tok0 + g;
-                        fk[0] = scale_60(sc[0]) * p.sl2; fk[1] = scale_60(sc[8]) * p.sl2;
-                        fv[0] = scale_60(sc[128]); fv[1] = scale_60(sc[136]);
+                        fk[0] = scale_of(sc[0]); fk[1] = scale_of(sc[8]);
+                        ev[0] = sc[128]; ev[1] = sc[136];
+                        // exponents of the V rows that the list has: highest (of the finite ones) and lowest
+                        const bool in0 = t0 + g < m.len, in1 = t0 + g + 8 < m.len;
+                        const int hi = __reduce_max_sync(0xffffffffu, max(in0 && ev[0] < 255 ? ev[0] : 0, in1 && ev[1] < 255 ? ev[1] : 0));
+                        const int lo = __reduce_min_sync(0xffffffffu, min(in0 ? ev[0] : 255, in1 ? ev[1] : 255));
+                        const bool nan = __any_sync(0xffffffffu, (in0 && ev[0] == 255) || (in1 && ev[1] == 255));
+                        if (e_ref < 0 || hi > e_ref + 4) {          // O follows: P stays below 2^12
+                            const float f = e_ref < 0 ? 0.f : pow2i(e_ref - hi);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) { o[nt][j][0] *= f; o[nt][j][1] *= f; o[nt][j][2] *= f; o[nt][j][3] *= f; }
+                            e_ref = hi;
+                        }
+                        classes = nan || lo < e_ref - 8;
+                        fv[0] = in0 ? pow2i(ev[0] - e_ref) : 0.f; fv[1] = in1 ? pow2i(ev[1] - e_ref) : 0.f;
                     }
                     uint32_t ph[NT][2], pl[NT][2];                  // P^T as B operands: high and low parts
                     float e[NT][4];
@@ -233,7 +275,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         float tm[2];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            float x = (s[nt][j] + s2[nt][j]) * fk[j >> 1];
+                            float x = (s[nt][j] + s2[nt][j]) * (E4M3 ? sl2[nt][j & 1] * fk[j >> 1] : p.sl2);
                             if (edge && t0 + g + 8 * (j >> 1) >= seen[nt][j & 1]) x = -INFINITY;
                             s[nt][j] = x;
                         }
@@ -258,13 +300,17 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             const float ref = mx[nt][j & 1];
                             const float x = fast_exp2(s[nt][j] - (ref == -INFINITY ? 0.f : ref));
                             l[nt][j & 1] += x;
-                            e[nt][j] = E4M3 ? (x > 0.f ? x * fv[j >> 1] : x) : x;          // (a NaN logit stays NaN; a token not seen has weight 0 whatever its scale)
+                            e[nt][j] = x;
                         }
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             uint32_t hi, lo;
-                            split_bf16x2(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
-                            ph[nt][j] = turned(hi); pl[nt][j] = turned(lo);
+                            if (E4M3) {
+                                ph[nt][j] = turned(pack_f16x2(e[nt][2 * j] * fv[j], e[nt][2 * j + 1] * fv[j]));
+                            } else {
+                                split_bf16x2(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
+                                ph[nt][j] = turned(hi); pl[nt][j] = turned(lo);
+                            }
                         }
                     }
                     if (!E4M3 && edge) {
@@ -307,20 +353,65 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             __syncwarp();
                         }
                     }
+                    if (E4M3 && t0 + 16 > m.len) {                  // rows behind the list's end may hold codes that stand for NaN
+                        const int row = tok0 + (lane >> 1);
+                        if (t0 + (lane >> 1) >= m.len) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(sv + row * 128 + (lane & 1) * 64 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
                     const int v_row = tok0 + (lane & 7) + (lane >> 4) * 8, v_pc = (lane >> 3) & 1;   // (tokens 0-7, p), (0-7, p + 1), (8-15, p), (8-15, p + 1)
                     if (E4M3) {
-#pragma unroll
-                        for (int pc = 0; pc < 8; pc += 2) {
-                            uint32_t r[4], a[4], b[4];
+                        auto v_pieces = [&](int pc, uint32_t (&a)[4], uint32_t (&b)[4]) {
+                            uint32_t r[4];
                             ldsm_x4_trans(r, sv + v_row * 128 + (((pc + v_pc) ^ (v_row & 7)) << 4));
                             expand_alternate(r[0], a[0], a[1]); expand_alternate(r[2], a[2], a[3]);      // piece pc: even channels, odd channels
                             expand_alternate(r[1], b[0], b[1]); expand_alternate(r[3], b[2], b[3]);
+                        };
+                        if (!classes) {
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_bf16(o[nt][pc], a, ph[nt][0], ph[nt][1]);
-                                mma_bf16(o[nt][pc + 1], b, ph[nt][0], ph[nt][1]);
-                                mma_bf16(o[nt][pc], a, pl[nt][0], pl[nt][1]);
-                                mma_bf16(o[nt][pc + 1], b, pl[nt][0], pl[nt][1]);
+                            for (int pc = 0; pc < 8; pc += 2) {
+                                uint32_t a[4], b[4];
+                                v_pieces(pc, a, b);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) {
+                                    mma_f16(o[nt][pc], a, ph[nt][0], ph[nt][1]);
+                                    mma_f16(o[nt][pc + 1], b, ph[nt][0], ph[nt][1]);
+                                }
+                            }
+                        } else {
+                            // tokens by classes of exponents, each with a reference of its own; a row of NaN (255) is seen by those whose weight is not 0
+                            bool todo[2] = {t0 + g < m.len, t0 + g + 8 < m.len};
+                            for (;;) {
+                                const int top = __reduce_max_sync(0xffffffffu, max(todo[0] ? ev[0] : -1, todo[1] ? ev[1] : -1));
+                                if (top < 0) break;
+                                const float back = top == 255 ? 1.f : pow2i(top - e_ref);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int j = 0; j < 2; ++j) {
+                                        const bool in = todo[j] && ev[j] > top - 10 && (top < 255 || ev[j] == 255);
+                                        const float f = top == 255 ? __uint_as_float(0x7fc00000u) : pow2i(ev[j] - top);
+                                        const float x = e[nt][2 * j], y = e[nt][2 * j + 1];
+                                        ph[nt][j] = turned(pack_f16x2(in && x != 0.f ? x * f : 0.f, in && y != 0.f ? y * f : 0.f));
+                                    }
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) todo[j] &= !(ev[j] > top - 10 && (top < 255 || ev[j] == 255));
+#pragma unroll
+                                for (int pc = 0; pc < 8; pc += 2) {
+                                    uint32_t a[4], b[4];
+                                    v_pieces(pc, a, b);
+#pragma unroll
+                                    for (int nt = 0; nt < NT; ++nt) {
+                                        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+                                        mma_f16(x, a, ph[nt][0], ph[nt][1]);
+                                        mma_f16(y, b, ph[nt][0], ph[nt][1]);
+#pragma unroll
+                                        for (int j = 0; j < 4; ++j) { o[nt][pc][j] = fmaf(x[j], back, o[nt][pc][j]); o[nt][pc + 1][j] = fmaf(y[j], back, o[nt][pc + 1][j]); }
+                                    }
+                                }
                             }
                         }
                     } else {
@@ -375,7 +466,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                     float top = -INFINITY;
 #pragma unroll
                     for (int w = 0; w < L::kWarps; ++w) top = fmaxf(top, sm[w * ROWS + nt * 8 + 2 * c + j]);
-                    f[nt][j] = exp2f(mx[nt][j] - (top == -INFINITY ? 0.f : top));
+                    f[nt][j] = exp2f(mx[nt][j] - (top == -INFINITY ? 0.f : top)) * (E4M3 ? (e_ref < 0 ? 1.f : pow2i(e_ref - 127)) : 1.f);
                 }
                 joined(nt * 8 + wg, ref_w[nt], sum_w[nt]);
             }
@@ -419,7 +510,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                     const float4 x = *reinterpret_cast<const float4*>(buf + (w * 8 + wg) * L::kPitch + lane * 4);
                     a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
                 }
-                const float sum = sum_w[nt], k = (E4M3 ? 0x1p60f : 1.f) * (whole ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
+                const float sum = sum_w[nt], k = whole ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f;
                 a.x *= k; a.y *= k; a.z *= k; a.w *= k;
                 if (whole) {
                     int head, i;

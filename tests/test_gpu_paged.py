@@ -155,7 +155,8 @@ def _attend(L, Hq, T, *, q_lens=None, causal=True, scale=0.0, seed=9, weight_bit
     return q, o, lse
 
 
-BITS = {"f32": 22, "bf16": 15, "e4m3": 15}           # weights of up to 16 rows per list: two bf16 parts
+# weights of up to 16 rows per list: fp32; two bf16 parts; fp16 (half a step of 2^-10, and 2^-25 of the largest where it is subnormal)
+BITS = {"f32": 22, "bf16": 15, "e4m3": 10.9}
 CHUNK_BITS = {"f32": 22, "bf16": 8, "e4m3": 8}       # of more rows: one bf16, off by half a step of 2^-7 at most
 
 
