@@ -438,7 +438,7 @@ obc_status obc_paged_write(const obc_pages* c, const obc_paged_write_params* p, 
     if ((st = check_tensor(k, true)) != OBC_OK) return st;
     if ((st = check_tensor(v, true)) != OBC_OK) return st;
     if (k.dtype != v.dtype) return OBC_ERR_UNSUPPORTED;
-    const PagedWrite w{p->rows, p->src_tokens, k.dtype, p->new_lens, p->new_lens_stride_b, p->new_lens_stride_h, p->idx};
+    const PagedWrite w{p->rows, p->src_tokens, k.dtype, FastDiv(p->rows), p->new_lens, p->new_lens_stride_b, p->new_lens_stride_h, p->idx};
     return launch_paged_write(pv, w, view(k), view(v), (cudaStream_t)stream);
 }
 

@@ -169,6 +169,7 @@ struct PagesView {                       // a paged cache as the kernels see it
 };
 struct PagedWrite {
     int rows, src_tokens, src_dtype;
+    FastDiv by_rows;
     const int32_t* new_lens; long long nb, nh;
     const int32_t* idx;
 };

@@ -219,7 +219,9 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
     char* w = static_cast<char*>(ws);
     AttnParams p{};
     p.c = c; p.G = s.G; p.T = s.T; p.causal = s.causal; p.q_lens = s.q_lens; p.sl2 = s.scale * kLog2e;
-    p.q = q; p.o = o; p.lse = lse; p.nrt = plan.nrt; p.items = plan.items;
+    p.q = q; p.o = o; p.lse = lse;
+    p.o_aligned = ((uintptr_t)o.ptr & 31) == 0 && o.sb % 16 == 0 && o.sh % 16 == 0 && o.st % 16 == 0;      // (elements of 2 bytes)
+    p.nrt = plan.nrt; p.items = plan.items;
     p.one_head = c.k.sh == 0 && c.v.sh == 0 ? 1 : 0;
     p.box = 8;
     p.box_shift = 3;

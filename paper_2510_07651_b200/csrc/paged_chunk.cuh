@@ -33,7 +33,7 @@ template <bool E4M3> struct ChunkLayout {
     static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
     static constexpr uint32_t kBad = kScales + kRaw * 128u;                            // [slot][4] words: tokens to be added by hand
     static constexpr uint32_t kBars = kBad + kSlots * 16u;
-    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PHALF = SFULL + 2, PFULL = PHALF + 2, TURN = PFULL + 2, ODONE = TURN + 8, RAWFULL = ODONE + 2,
+    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PFULL = SFULL + 2, TURN = PFULL + 2, ODONE = TURN + 8, RAWFULL = ODONE + 2,
            RAWEMPTY = RAWFULL + 2, NBARS = RAWEMPTY + 2 };
     static constexpr uint32_t kTmem = kBars + NBARS * 8u;
     static constexpr uint32_t kSmem = kTmem + 16 + 1024;
@@ -69,6 +69,10 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void tc_ld1(uint32_t taddr, uint32_t& r) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(r) : "r"(taddr) : "memory");
 }
+// 32 bytes in one store (a whole sector; two stores of 16 bytes by each of 32 lanes in rows of their own take twice the requests)
+__device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, uint32_t e, uint32_t f, uint32_t g, uint32_t h) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a), "r"(b), "r"(c), "r"(d), "r"(e), "r"(f), "r"(g), "r"(h) : "memory");
+}
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 // four bytes (e4m3 codes) -> two bf16 pairs, times m1 * m2 (powers of two that leave the product exact)
@@ -98,7 +102,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
         for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 2); mbar_init(bar(L::EDGE + i), 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PHALF + i), 4); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
+            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
             mbar_init(bar(L::RAWFULL + i), 33); mbar_init(bar(L::RAWEMPTY + i), 4);
         }
         for (int i = 0; i < 8; ++i) mbar_init(bar(L::TURN + i), 1);
@@ -216,17 +220,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     if (!all_wait(L::FULL + slot, phase, __LINE__)) break;
                     if (i < cnt) {
                         const uint32_t av = desc_lo_mn(sbase + L::kRing + slot * kOperandBytes);
+                        if (!all_wait(L::PFULL + w, np, __LINE__)) break;
+                        tc_fence_after();
+                        if (leader) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {                            // 64 tokens of P at a time, as they come
-                            if (!all_wait((h ? L::PFULL : L::PHALF) + w, np, __LINE__)) break;
-                            tc_fence_after();
-                            if (leader) {
-#pragma unroll
-                                for (int ks = 4 * h; ks < 4 * h + 4; ++ks)       // steps of K = 16 tokens (2048 bytes of V each)
-                                    tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
-                            }
+                            for (int ks = 0; ks < 8; ++ks)               // steps of K = 16 tokens (2048 bytes of V each)
+                                tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
                         }
-                        if (fail_site) break;
                         ++np;
                         if (leader) {
                             tc_commit(bar(L::EMPTY + slot));
@@ -294,14 +294,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         // Q of a segment: sixteen lanes per row; rows that are not there become zeros.  Asked for as soon as the segment before has its last logits.
         auto ask_q = [&](const Item& m) {
             const int tid = lane_grp * 32 + lane, piece = tid & 15;
+            int head = 0, i = 0;
+            row_place(p, m, w * 128 + (tid >> 4), head, i);         // eight rows further on: di queries and dg heads
+            const int g0 = m.h * p.G, di = p.by_G.div(8), dg = 8 - di * p.G;
+            int g = head - g0;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.ptr) + m.b * p.q.sb + head * p.q.sh + i * p.q.st + piece * 8;
+            const long long step = di * p.q.st + dg * p.q.sh, wrap = p.q.st - p.G * p.q.sh;
+            const uint32_t dst = sbase + L::kQ + w * kOperandBytes + (piece >> 3) * kHalfBytes;
 #pragma unroll 4
             for (int rr = tid >> 4; rr < 128; rr += 8) {
                 const bool there = w * 128 + rr < m.rows;
-                int head = 0, i = 0;
-                if (there) row_place(p, m, w * 128 + rr, head, i);
-                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q.ptr) + (there ? m.b * p.q.sb + head * p.q.sh + i * p.q.st : 0) + piece * 8;
-                const uint32_t dst = sbase + L::kQ + w * kOperandBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)),
+                             "l"(there ? src : static_cast<const __nv_bfloat16*>(p.q.ptr)), "r"(there ? 16 : 0) : "memory");
+                src += step; g += dg;
+                if (g >= p.G) { g -= p.G; src += wrap; }
             }
         };
         auto q_there = [&]() {
@@ -318,6 +324,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const Item m = seg.m;
             const ChunkSeg c = chunk_seg(p, seg);
             const int cnt = c.cnt(w), both = min(c.cnt0, c.cnt1), seen = seen_by(p, m, r), ta = seg.ta;
+            const bool whole = seg.whole(), there = r < m.rows;
+            const size_t at = seg.slot() * kChunkRows + r;
+            int head = 0, iq = 0;
+            if (there) row_place(p, m, r, head, iq);
+            __nv_bfloat16* const dst = static_cast<__nv_bfloat16*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + iq * p.o.st;
+            const int lse_at = (m.b * p.c.Hkv * p.G + head) * p.T + iq;
+            info = seg.shared_item(run);
+            more = seg.next();                                      // (looked up while the first logits are on their way)
+            const bool next_q = more && chunk_seg(p, seg).cnt(w) > 0;
             float m_used = -INFINITY, l = 0.f;
             if (cnt > 0) {                                          // O starts at 0 (all of its MMAs accumulate)
                 uint32_t z[32];
@@ -393,12 +408,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             pk[j >> 1] = pack_bf16x2(ex.x, ex.y);
                         }
                         tc_st16(tS + q * 16, pk);
-                        if (q == 1 && !edge) {                      // the MMAs may have the first 64 tokens
-                            tc_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(bar(L::PHALF + w));
-                        }
                     }
                     if (i < both && lane == 0) mbar_arrive(bar(L::TURN + 4 * (w ^ 1) + lane_grp));
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
@@ -437,19 +446,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        if (edge) mbar_arrive(bar(L::PHALF + w));
-                        mbar_arrive(bar(L::PFULL + w));
-                    }
+                    if (lane == 0) mbar_arrive(bar(L::PFULL + w));
                 }
             }
             base += c.n;
             if (fail_site) break;
-            const bool whole = seg.whole(), there = r < m.rows;
-            const size_t at = seg.slot() * kChunkRows + r;
-            info = seg.shared_item(run);
-            more = seg.next();
-            const bool next_q = more && chunk_seg(p, seg).cnt(w) > 0;
             if (next_q) ask_q(seg.m);
             // ---- the segment's result ----
             if (cnt > 0) {
@@ -458,9 +459,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 tc_fence_after();
             }
             const float k = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
-            int head = 0, iq = 0;
-            if (there) row_place(p, m, r, head, iq);
-            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(const_cast<void*>(p.o.ptr)) + m.b * p.o.sb + head * p.o.sh + iq * p.o.st;
             if (cnt > 0 || whole) {
 #pragma unroll 1
                 for (int q = 0; q < 4; ++q) {
@@ -474,21 +472,28 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                     if (!there) continue;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        float f[8];
+                    for (int j = 0; j < 32; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * k);
+                    if (whole) {
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(ov[j + x]) * k;
-                        if (whole) {
-                            *reinterpret_cast<uint4*>(dst + q * 32 + j) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-                        } else {
-                            float4* po = reinterpret_cast<float4*>(p.part_o + at * kD + q * 32 + j);
-                            po[0] = make_float4(f[0], f[1], f[2], f[3]);
-                            po[1] = make_float4(f[4], f[5], f[6], f[7]);
+                        for (int j = 0; j < 32; j += 16) {
+                            uint32_t h[8];
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) h[x] = pack_bf16x2(__uint_as_float(ov[j + 2 * x]), __uint_as_float(ov[j + 2 * x + 1]));
+                            if (p.o_aligned) {
+                                store32(dst + q * 32 + j, h[0], h[1], h[2], h[3], h[4], h[5], h[6], h[7]);
+                            } else {
+                                *reinterpret_cast<uint4*>(dst + q * 32 + j) = make_uint4(h[0], h[1], h[2], h[3]);
+                                *reinterpret_cast<uint4*>(dst + q * 32 + j + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+                            }
                         }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            store32(p.part_o + at * kD + q * 32 + j, ov[j], ov[j + 1], ov[j + 2], ov[j + 3], ov[j + 4], ov[j + 5], ov[j + 6], ov[j + 7]);
                     }
                 }
             }
-            if (there && whole && p.lse) p.lse[((size_t)m.b * p.c.Hkv * p.G + head) * p.T + iq] = lse_of(m_used == -INFINITY ? 0.f : m_used, l);
+            if (there && whole && p.lse) p.lse[lse_at] = lse_of(m_used == -INFINITY ? 0.f : m_used, l);
             if (there && !whole) { p.part_m[at] = m_used; p.part_l[at] = l; }
             tc_fence_before();                                      // (O is read: the next segment's MMAs follow the next P's barrier)
             if (next_q) q_there();
@@ -517,10 +522,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::RAWEMPTY + st));
-                    // code bits are the value times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range
+                    // code bits are the value (finite, whatever the code) times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range; 0 for rows that become zeros
                     const bool nan = s > 186u, odd = op && nan && t >= c.first_masked && t < seg.m.len, gone = op && (odd || t >= seg.m.len);
                     const int e1 = min((int)s - 7, 127), e2 = (int)s - 7 - e1;
-                    const __nv_bfloat16 f1 = nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
+                    const __nv_bfloat16 f1 = gone ? __float2bfloat16(0.f) : nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
                     const __nv_bfloat16 f2 = __float2bfloat16(__uint_as_float((uint32_t)(min(e2, 127) + 127) << 23));
                     const __nv_bfloat162 m1 = __halves2bfloat162(f1, f1), m2 = __halves2bfloat162(f2, f2);
                     if (!all_wait(L::EMPTY + slot, (n / NS) ^ 1u, __LINE__)) break;
@@ -531,7 +536,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         uint4 y;
                         codes_to_bf16(j & 1 ? x[j >> 1].z : x[j >> 1].x, m1, m2, two, y.x, y.y);
                         codes_to_bf16(j & 1 ? x[j >> 1].w : x[j >> 1].y, m1, m2, two, y.z, y.w);
-                        if (gone) y = make_uint4(0u, 0u, 0u, 0u);
                         *reinterpret_cast<uint4*>(dst + (j >> 3) * kHalfBytes + (((j & 7) ^ sw) << 4)) = y;
                     }
                     const uint32_t word = __ballot_sync(0xffffffffu, odd);

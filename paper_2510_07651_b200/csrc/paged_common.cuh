@@ -22,6 +22,7 @@ struct AttnParams {
     const int32_t* q_lens;
     float sl2;                               // scale * log2(e)
     TensorView q, o;
+    int o_aligned;                           // rows of o begin on 32-byte boundaries
     float* lse;                              // or nullptr
     int nrt, items;                          // row tiles per list, items in all
     FastDiv by_G, by_nrt;
@@ -66,7 +67,7 @@ __device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0
 // natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)
 __device__ __forceinline__ float lse_of(float ref, float total) { return (ref + log2f(total)) * 0.6931471805599453f; }
 
-constexpr int kSegCost = 2;
+constexpr int kSegCost = 3;
 
 struct Run { int begin, end, size, longer; int item, off; };      // runs of size + 1 (the first `longer`) and of size
 struct RunScratch { int warp_sum[32]; int item, off; };
