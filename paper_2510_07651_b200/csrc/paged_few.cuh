@@ -9,7 +9,7 @@
 // per tile, hence two groups of eight warps on alternate tiles where the registers allow it (8 rows).
 //
 // e4m3 rows become fp16 in registers, which holds every code exactly (one conversion for two codes; to bf16 it took seven instructions for
-// four and, since P then needs two parts, twice the MMAs: 256 lists of 4096 tokens 80 us against 62).  The channels of a 16-channel step are
+// four and, since P then needs two parts, twice the MMAs: 256 lists of 4096 tokens 80 us against 76).  The channels of a 16-channel step are
 // taken in the order in which ldmatrix hands out their bytes (q is loaded in the same order), and the rows of an O^T tile are eight even and
 // eight odd channels.  q is scaled by a power of two per row, so that its largest value is near 2^14 (what falls below fp16's range is less
 // than 2^-38 of it).  The scale of a K row goes into its logit, that of a V row into its P, relative to a reference exponent that O carries: P is
@@ -26,9 +26,9 @@ namespace {
 template <int NT, bool E4M3> struct FewLayout {
     static constexpr int kRows = 8 * NT, kGroups = NT == 1 ? 2 : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 64;
     static constexpr uint32_t kOperand = kTokTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
-    static constexpr int kStages = E4M3 ? 5 : 3, kFull = kStages * kGroups;
+    static constexpr int kStages = E4M3 ? 6 : 3, kFull = kStages * kGroups;
     static constexpr int kPitch = kD + 4;                                                  // floats per row of O in the merge buffer
-    static constexpr uint32_t kMerge = kStages * kStage, kMergeBytes = 8 * 8 * kPitch * 4;
+    static constexpr uint32_t kMerge = kStages * kStage, kMergeBytes = 4 * 8 * kPitch * 4;
     static constexpr uint32_t kScales = kMerge + kMergeBytes;                              // [stage][K, V][128] scale bytes
     static constexpr uint32_t kBars = kScales + (E4M3 ? (uint32_t)kStages * 256u : 0u);    // full, empty
     static constexpr uint32_t kSmem = kBars + (kFull + kStages) * 8u + 1024;               // + alignment slack
@@ -471,34 +471,26 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 joined(nt * 8 + wg, ref_w[nt], sum_w[nt]);
             }
             const bool whole = seg.whole();
-            float* buf = reinterpret_cast<float*>(smem + L::kMerge);           // [warp of the group][row][channel]
-            auto put = [&](int nt) {
-                float* at = buf + wg * 8 * L::kPitch + 2 * c * L::kPitch;
+            float* buf = reinterpret_cast<float*>(smem + L::kMerge);           // [four warps][row][channel]
+            // four warps at a time, the last four first, the others adding to what they find
+            auto put = [&](int nt, bool add) {
+                float* at = buf + (warp & 3) * 8 * L::kPitch + 2 * c * L::kPitch;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int ch = 16 * j + (E4M3 ? 2 * g : g), up = E4M3 ? 1 : 8;
-                    at[ch] = o[nt][j][0] * f[nt][0]; at[L::kPitch + ch] = o[nt][j][1] * f[nt][1];
-                    at[ch + up] = o[nt][j][2] * f[nt][0]; at[L::kPitch + ch + up] = o[nt][j][3] * f[nt][1];
-                }
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        float* to = at + (x & 1) * L::kPitch + 16 * j + (E4M3 ? 2 * g + (x >> 1) : g + 8 * (x >> 1));
+                        const float v = o[nt][j][x] * f[nt][x & 1];
+                        *to = add ? *to + v : v;
+                    }
             };
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 if (nt * 8 >= m.rows) break;
-                consumers_sync<CONS>();                             // the buffer is free (again)
-                if (L::kGroups == 2) {                              // the second group's first, added to by the first group in place
-                    if (group == 1) put(nt);
-                    consumers_sync<CONS>();
-                    if (group == 0) {
-                        float* at = buf + wg * 8 * L::kPitch + 2 * c * L::kPitch;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int ch = 16 * j + (E4M3 ? 2 * g : g), up = E4M3 ? 1 : 8;
-                            at[ch] += o[nt][j][0] * f[nt][0]; at[L::kPitch + ch] += o[nt][j][1] * f[nt][1];
-                            at[ch + up] += o[nt][j][2] * f[nt][0]; at[L::kPitch + ch + up] += o[nt][j][3] * f[nt][1];
-                        }
-                    }
-                } else {
-                    put(nt);
+#pragma unroll 1
+                for (int k = L::kWarps / 4 - 1; k >= 0; --k) {
+                    consumers_sync<CONS>();                         // (before the first: the buffer is free)
+                    if (warp >> 2 == k) put(nt, k < L::kWarps / 4 - 1);
                 }
                 consumers_sync<CONS>();
                 // a warp of the first group sums and stores one row
@@ -506,7 +498,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 if (group != 0 || r >= m.rows) continue;
                 float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < 8; ++w) {
+                for (int w = 0; w < 4; ++w) {
                     const float4 x = *reinterpret_cast<const float4*>(buf + (w * 8 + wg) * L::kPitch + lane * 4);
                     a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
                 }
