@@ -192,7 +192,7 @@ AttnPlan make_plan(const PagesView& c, const AttnShape& s) {
     AttnPlan p{};
     const long long rows = (long long)s.G * s.T;
     p.rows = c.dtype == OBC_F32 ? kF32Rows : rows <= 8 ? 8 : rows <= 16 ? 16 : kChunkRows;
-    p.grid = sm_count() * (c.dtype == OBC_F32 ? 2 : 1);
+    p.grid = sm_count() * (c.dtype == OBC_F32 ? 2 : c.dtype == OBC_E4M3 && p.rows == 8 ? FewLayout<1, true>::kCtas : 1);
     p.nrt = (int)((rows + p.rows - 1) / p.rows);
     p.items = c.B * c.Hkv * p.nrt;
     size_t off = 256;                                  // header: the status word

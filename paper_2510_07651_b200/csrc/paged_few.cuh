@@ -24,11 +24,13 @@ namespace obc {
 namespace {
 
 template <int NT, bool E4M3> struct FewLayout {
-    static constexpr int kRows = 8 * NT, kGroups = NT == 1 ? 2 : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 64;
+    static constexpr int kRows = 8 * NT, kCtas = E4M3 && NT == 1 ? 2 : 1;                   // CTAs per SM
+    static constexpr int kGroups = NT == 1 ? 2 / kCtas : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 64;
     static constexpr uint32_t kOperand = kTokTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
-    static constexpr int kStages = E4M3 ? 6 : 3, kFull = kStages * kGroups;
+    static constexpr int kStages = E4M3 ? 6 / kCtas : 3, kFull = kStages * kGroups;
+    static constexpr int kSlots = 4 / kCtas;                                               // warps whose O the merge buffer holds
     static constexpr int kPitch = kD + 4;                                                  // floats per row of O in the merge buffer
-    static constexpr uint32_t kMerge = kStages * kStage, kMergeBytes = 4 * 8 * kPitch * 4;
+    static constexpr uint32_t kMerge = kStages * kStage, kMergeBytes = kSlots * 8 * kPitch * 4;
     static constexpr uint32_t kScales = kMerge + kMergeBytes;                              // [stage][K, V][128] scale bytes
     static constexpr uint32_t kBars = kScales + (E4M3 ? (uint32_t)kStages * 256u : 0u);    // full, empty
     static constexpr uint32_t kSmem = kBars + (kFull + kStages) * 8u + 1024;               // + alignment slack
@@ -124,7 +126,7 @@ __device__ __forceinline__ uint32_t few_piece(int box_shift, int row, int piece)
 }
 
 template <int NT, bool E4M3>
-__global__ void __launch_bounds__(FewLayout<NT, E4M3>::kThreads, 1)
+__global__ void __launch_bounds__(FewLayout<NT, E4M3>::kThreads, FewLayout<NT, E4M3>::kCtas)
 few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnParams p) {
     using L = FewLayout<NT, E4M3>;
     constexpr int ROWS = L::kRows, CONS = 32 * L::kWarps;
@@ -471,10 +473,10 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 joined(nt * 8 + wg, ref_w[nt], sum_w[nt]);
             }
             const bool whole = seg.whole();
-            float* buf = reinterpret_cast<float*>(smem + L::kMerge);           // [four warps][row][channel]
-            // four warps at a time, the last four first, the others adding to what they find
+            float* buf = reinterpret_cast<float*>(smem + L::kMerge);           // [warp][row][channel]
+            // as many warps at a time as there is room for, the last ones first, the others adding to what they find
             auto put = [&](int nt, bool add) {
-                float* at = buf + (warp & 3) * 8 * L::kPitch + 2 * c * L::kPitch;
+                float* at = buf + warp % L::kSlots * 8 * L::kPitch + 2 * c * L::kPitch;
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -488,9 +490,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             for (int nt = 0; nt < NT; ++nt) {
                 if (nt * 8 >= m.rows) break;
 #pragma unroll 1
-                for (int k = L::kWarps / 4 - 1; k >= 0; --k) {
+                for (int k = L::kWarps / L::kSlots - 1; k >= 0; --k) {
                     consumers_sync<CONS>();                         // (before the first: the buffer is free)
-                    if (warp >> 2 == k) put(nt, k < L::kWarps / 4 - 1);
+                    if (warp / L::kSlots == k) put(nt, k < L::kWarps / L::kSlots - 1);
                 }
                 consumers_sync<CONS>();
                 // a warp of the first group sums and stores one row
@@ -498,7 +500,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 if (group != 0 || r >= m.rows) continue;
                 float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < L::kSlots; ++w) {
                     const float4 x = *reinterpret_cast<const float4*>(buf + (w * 8 + wg) * L::kPitch + lane * 4);
                     a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
                 }
