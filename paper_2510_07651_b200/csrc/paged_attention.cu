@@ -192,7 +192,7 @@ AttnPlan make_plan(const PagesView& c, const AttnShape& s) {
     AttnPlan p{};
     const long long rows = (long long)s.G * s.T;
     p.rows = c.dtype == OBC_F32 ? kF32Rows : rows <= 8 ? 8 : rows <= 16 ? 16 : kChunkRows;
-    p.grid = sm_count() * (c.dtype == OBC_F32 ? 2 : c.dtype == OBC_E4M3 && p.rows == 8 ? FewLayout<1, true>::kCtas : 1);
+    p.grid = sm_count() * (c.dtype == OBC_F32 || p.rows == 8 ? 2 : 1);
     p.nrt = (int)((rows + p.rows - 1) / p.rows);
     p.items = c.B * c.Hkv * p.nrt;
     size_t off = 256;                                  // header: the status word
@@ -223,9 +223,9 @@ obc_status launch_paged_attention(const PagesView& c, const AttnShape& s, Tensor
     p.o_aligned = ((uintptr_t)o.ptr & 31) == 0 && o.sb % 16 == 0 && o.sh % 16 == 0 && o.st % 16 == 0;      // (elements of 2 bytes)
     p.nrt = plan.nrt; p.items = plan.items;
     p.one_head = c.k.sh == 0 && c.v.sh == 0 ? 1 : 0;
-    p.box = 8;
-    p.box_shift = 3;
-    while (p.box < kTokTile && c.P % (2 * p.box) == 0) { p.box *= 2; ++p.box_shift; }
+    const int tile = c.dtype == OBC_BF16 && plan.rows == 8 ? FewLayout<1, false>::kTile : kTokTile;
+    p.box = 8; p.box_shift = 3;
+    while (p.box < tile && c.P % (2 * p.box) == 0) { p.box *= 2; ++p.box_shift; }
     p.by_G = FastDiv(s.G); p.by_nrt = FastDiv(plan.nrt);
     p.status = reinterpret_cast<unsigned int*>(w);
     p.info = reinterpret_cast<int4*>(w + plan.off_info);

@@ -151,18 +151,21 @@ struct Segments {
 };
 
 // The tiles of a CTA's run, for the warp that asks for their pages.  A lane holds the page number of one box in a window of 32
-// consecutive boxes (a tile has 128 / box <= 16 of them, so it lies within one window); the next window's, or the next segment's first,
+// consecutive boxes (a tile has at most 16 of them, so it lies within one window); the next window's, or the next segment's first,
 // travel while the current ones are used.  (With the numbers of one tile at a time, asked for one tile ahead, 32 sequences of up
 // to 8192 tokens took 124 us against 97 without any look-up.)
-template <int ROWS>
+template <int ROWS, int TILE_TOKENS = kTokTile>
 struct TileWalk {
+    static constexpr int kParts = kTokTile / TILE_TOKENS;      // tiles of the walk in one of a segment's
+    static constexpr int kBits = TILE_TOKENS == 128 ? 7 : 6;
+    static_assert(TILE_TOKENS == 1 << kBits, "tile");
     const AttnParams& p;
     Segments<ROWS> cur, nxt;
     bool more, more_next;
     int lane, tile, pages, pages_next;
-    int slot, slot8, step;                   // places in their pages of the lane's box and of the lane's eight tokens (of 16 lanes); 128 mod P
+    int slot, slot8, step;                   // places in their pages of the lane's box and of the lane's eight tokens (of 16 lanes); a tile's tokens mod P
     __device__ __forceinline__ TileWalk(const AttnParams& p_, const Run& r, int lane_) : p(p_), cur(p_, r), nxt(p_, r), lane(lane_) {
-        step = p.c.by_P.mod(kTokTile);
+        step = p.c.by_P.mod(TILE_TOKENS);
         more = cur.next();
         pages = pages_next = -1;
         more_next = false;
@@ -174,11 +177,11 @@ struct TileWalk {
         nxt.copy(cur); more_next = nxt.next();
         ahead();
     }
-    __device__ __forceinline__ int boxes() const { return kTokTile >> p.box_shift; }
-    __device__ __forceinline__ int window(int t) const { return t >> (p.box_shift - 2); }                  // 32 boxes = 2^(shift + 5) tokens
+    __device__ __forceinline__ int boxes() const { return TILE_TOKENS >> p.box_shift; }
+    __device__ __forceinline__ int window(int t) const { return t >> (p.box_shift + 5 - kBits); }         // 32 boxes = 2^(shift + 5) tokens
     __device__ __forceinline__ void begin() {
-        tile = cur.ta;
-        slot = p.c.by_P.mod(tile * kTokTile + (lane << p.box_shift)); slot8 = p.c.by_P.mod(tile * kTokTile + (lane & 15) * 8);
+        tile = cur.ta * kParts;
+        slot = p.c.by_P.mod(tile * TILE_TOKENS + (lane << p.box_shift)); slot8 = p.c.by_P.mod(tile * TILE_TOKENS + (lane & 15) * 8);
     }
     __device__ __forceinline__ int asked(const Item& m, int win) const {
         const int t = (win * 32 + lane) << p.box_shift;
@@ -187,8 +190,8 @@ struct TileWalk {
         return v;
     }
     __device__ __forceinline__ void ahead() {
-        if (window(tile) < window(cur.tb - 1)) pages_next = asked(cur.m, window(tile) + 1);
-        else if (more_next) pages_next = asked(nxt.m, window(nxt.ta));
+        if (window(tile) < window(cur.tb * kParts - 1)) pages_next = asked(cur.m, window(tile) + 1);
+        else if (more_next) pages_next = asked(nxt.m, window(nxt.ta * kParts));
     }
     // page of the lane's box of the current tile; -1 for rows of zeros (behind the list, or a page that is not there)
     __device__ __forceinline__ int page() const {
@@ -196,7 +199,7 @@ struct TileWalk {
         return lane < boxes() && (unsigned)v < (unsigned)p.c.n_pages ? v : -1;
     }
     __device__ __forceinline__ void advance() {
-        if (++tile < cur.tb) {
+        if (++tile < cur.tb * kParts) {
             slot += step; slot8 += step;
             if (slot >= p.c.P) slot -= p.c.P;
             if (slot8 >= p.c.P) slot8 -= p.c.P;

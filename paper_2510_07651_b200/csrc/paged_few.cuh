@@ -5,8 +5,9 @@
 //     S^T = K q^T      16 tokens x 8 rows, 8 steps of 16 channels
 //     O^T += V^T P^T   16 channels x 8 rows, 8 tiles, one step of 16 tokens; P^T is S^T's accumulator turned by movmatrix
 // A warp keeps (m, l, O) of its own tokens; they meet once per segment.  P enters as bf16(P) + bf16(P - bf16(P)), so that o is off by no
-// more than its own rounding (the MMAs are nowhere near their limit here).  What sets the pace is the chain of dependent steps of a warp
-// per tile, hence two groups of eight warps on alternate tiles where the registers allow it (8 rows).
+// more than its own rounding (the MMAs are nowhere near their limit here).  With up to 8 rows two CTAs share an SM, so that one's segment
+// beginnings and ends (q, the joining of its warps' results) hide behind the other's tiles: 256 lists of 4096 tokens in 8 bits 74 -> 65 us.
+// Tiles of 16-bit rows are halved for it (three stages of 64 tokens each).
 //
 // e4m3 rows become fp16 in registers, which holds every code exactly (one conversion for two codes; to bf16 it took seven instructions for
 // four and, since P then needs two parts, twice the MMAs: 256 lists of 4096 tokens 80 us against 76).  The channels of a 16-channel step are
@@ -24,9 +25,10 @@ namespace obc {
 namespace {
 
 template <int NT, bool E4M3> struct FewLayout {
-    static constexpr int kRows = 8 * NT, kCtas = E4M3 && NT == 1 ? 2 : 1;                   // CTAs per SM
-    static constexpr int kGroups = NT == 1 ? 2 / kCtas : 1, kWarps = 8 * kGroups, kThreads = 32 * kWarps + 64;
-    static constexpr uint32_t kOperand = kTokTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
+    static constexpr int kRows = 8 * NT, kCtas = NT == 1 ? 2 : 1;                          // CTAs per SM
+    static constexpr int kTile = !E4M3 && NT == 1 ? 64 : kTokTile;                         // tokens per stage
+    static constexpr int kWarps = 8, kPerTile = kTile / 16, kGroups = kWarps / kPerTile, kThreads = 32 * kWarps + 64;
+    static constexpr uint32_t kOperand = kTile * (E4M3 ? 128u : 256u), kStage = 2 * kOperand;
     static constexpr int kStages = E4M3 ? 6 / kCtas : 3, kFull = kStages * kGroups;
     static constexpr int kSlots = 4 / kCtas;                                               // warps whose O the merge buffer holds
     static constexpr int kPitch = kD + 4;                                                  // floats per row of O in the merge buffer
@@ -142,7 +144,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
         for (int i = 0; i < L::kFull; ++i) mbar_init(full(i), E4M3 ? 66 : 2);
-        for (int i = 0; i < L::kStages; ++i) mbar_init(empty(i), 8);
+        for (int i = 0; i < L::kStages; ++i) mbar_init(empty(i), L::kPerTile);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
@@ -153,7 +155,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     if (warp >= L::kWarps) {
         // ============================ producers: a warp for K, one for V =====================
         const bool is_v = warp > L::kWarps;
-        TileWalk<ROWS> walk(p, run, lane);
+        TileWalk<ROWS, L::kTile> walk(p, run, lane);
         int n = 0, st = 0, fb = 0;                                  // tiles issued; stage and barrier of the next
         uint32_t phase = 1;
         while (walk.more) {
@@ -171,8 +173,8 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         }
     } else {
         // ===================================== consumers ====================================
-        const int g = lane >> 2, c = lane & 3, group = warp >> 3, wg = warp & 7;
-        const int tok0 = wg * 16;                                   // the warp's tokens of a tile
+        const int g = lane >> 2, c = lane & 3, group = warp / L::kPerTile, wg = warp;
+        const int tok0 = warp % L::kPerTile * 16;                   // the warp's tokens of a tile
         Segments<ROWS> seg(p, run);
         int4 info = make_int4(-1, 0, 0, 0);
         int st = 0, fb = 0, turn = 0;                               // stage, barrier and group of the next tile
@@ -203,18 +205,19 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
             }
             const int first_masked = p.causal ? min(max(m.len - m.ql + p.by_G.div(m.r0) + 1, 0), m.len) : m.len;   // tokens that not every row sees begin here
 
-            for (int tile = seg.ta; tile < seg.tb; ++tile) {
+            constexpr int kParts = kTokTile / L::kTile;
+            for (int tile = seg.ta * kParts; tile < seg.tb * kParts; ++tile) {
                 const bool mine = L::kGroups == 1 || turn == group;
                 const int s_at = st, f_at = fb;
                 const uint32_t par = phase;
-                turn ^= 1;
+                if (++turn == L::kGroups) turn = 0;
                 if (++st == L::kStages) st = 0;
                 if (++fb == L::kFull) { fb = 0; phase ^= 1u; }
                 if (!mine) continue;
                 uint8_t* sk = smem + s_at * L::kStage;
                 uint8_t* sv = sk + L::kOperand;
                 if (!__all_sync(0xffffffffu, mbar_wait(full(f_at), par))) { fail_site = __LINE__; break; }
-                const int t0 = tile * kTokTile + tok0;              // the warp's first token
+                const int t0 = tile * L::kTile + tok0;              // the warp's first token
                 const bool edge = t0 + 16 > first_masked;           // some row does not see some of the 16 tokens
                 if (t0 < m.len) {
                     float s[NT][4], s2[NT][4];                      // even and odd steps: half the chain
@@ -495,9 +498,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                     if (warp / L::kSlots == k) put(nt, k < L::kWarps / L::kSlots - 1);
                 }
                 consumers_sync<CONS>();
-                // a warp of the first group sums and stores one row
+                // a warp sums and stores one row
                 const int r = nt * 8 + wg;
-                if (group != 0 || r >= m.rows) continue;
+                if (r >= m.rows) continue;
                 float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < L::kSlots; ++w) {
