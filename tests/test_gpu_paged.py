@@ -281,6 +281,17 @@ def test_chunks_of_a_padded_batch(pages):
 
 
 @pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq", [2, 8, 14, 32])
+def test_single_tokens_beside_chunks(pages, Hq):
+    """Lists of few rows, of the most that the kernel for few takes (and one more), and of many in one call, long and short ones of each."""
+    q_lens = [1, 8, 100, 1, 9, 0, 2, 300, 1, 4]
+    L = Lists([9000, 700, 800, 1, 64, 50, 3000, 300, 17, 4], 2, 16, pages, seed=Hq)
+    _attend(L, Hq, 300, q_lens=q_lens, weight_bits=8)
+    _attend(L, Hq, 300, q_lens=[1] * 10, weight_bits=8)
+    _attend(L, Hq, 300, q_lens=[0] * 10, weight_bits=8)
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
 @pytest.mark.parametrize("spread", [2, 12])
 def test_chunks_of_different_magnitude(pages, spread):
     _attend(Lists([700, 77], 2, 16, pages, seed=1, spread=spread), 8, 60, weight_bits=8)
