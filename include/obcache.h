@@ -355,7 +355,7 @@ obc_status obc_decode_step(const obc_decode_params* p, obc_tensor q_t, obc_tenso
  * ------------------------------------------------------------------------------------------ */
 typedef struct {
     size_t struct_size;
-    obc_tensor k, v;           /* [n_pages, n_kv_heads or 1, page_size, d]: stride_b goes from page to page */
+    obc_tensor k, v;           /* [n_pages, n_kv_heads or 1, page_size, d]: stride_b goes from page to page (not 0) */
     uint8_t* k_scale;          /* device, e4m3 only (else NULL): biased exponents, tokens of a page contiguous */
     uint8_t* v_scale;
     int64_t scale_stride_p, scale_stride_h;   /* from page to page, from head to head; multiples of 8 */
@@ -397,7 +397,7 @@ obc_status obc_paged_read(const obc_pages* c, int32_t n_tokens, obc_tensor k_out
  * rows are in the cache already (obc_paged_write), as the last q_len tokens of their lists.  Query i = 0..q_len-1 of batch item b
  * sees the tokens p <= len - q_len + i of its KV head's list (all p < len unless causal):
  *   Z_ip = scale * q_i . k_p;   lse_i = log sum_p exp Z_ip;   o_i = sum_p exp(Z_ip - lse_i) v_p
- * A query that sees nothing has o = 0 and lse = -inf.  o and lse are what obc_score_given takes.
+ * A query that sees nothing, or finite rows of V with logits of -inf only, has o = 0 and lse = -inf.  o and lse are what obc_score_given takes.
  *   q, o   [B,Hq,n_tokens,d], one type: f32 over f32 pages, bf16 over bf16 or e4m3 pages
  *   lse    device fp32 [B,Hq,n_tokens] contiguous, or NULL
  * Rows i >= q_len of o and lse are left as they are.  Sums and softmax statistics are fp32.  Infinities and NaN are no

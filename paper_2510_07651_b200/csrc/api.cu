@@ -413,6 +413,7 @@ static obc_status resolve_pages(const obc_pages* c, PagesView* v) {
     obc_status st;
     if ((st = check_pages_tensor(c->k, dtype)) != OBC_OK) return st;
     if ((st = check_pages_tensor(c->v, dtype)) != OBC_OK) return st;
+    if (c->n_pages > 1 && (c->k.stride_b == 0 || c->v.stride_b == 0)) return OBC_ERR_SHAPE;       // (a bulk copy's descriptor knows no stride of 0)
     if (c->n_kv_heads > 1 && (c->k.stride_h == 0) != (c->v.stride_h == 0)) return OBC_ERR_SHAPE;
     if ((dtype == OBC_E4M3) != (c->k_scale != nullptr) || (dtype == OBC_E4M3) != (c->v_scale != nullptr)) return dtype == OBC_E4M3 ? OBC_ERR_NULL : OBC_ERR_UNSUPPORTED;
     if (dtype == OBC_E4M3) {

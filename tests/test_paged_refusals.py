@@ -44,7 +44,7 @@ BAD_PAGES = [
     (dict(page_size=4), -2), (dict(max_pages=0), -2), (dict(max_pages=1 << 27), -2), (dict(batch=40000), -2), (dict(table=None), -1), (dict(lens=None), -1),
     (dict(table=4098), -4), (dict(lens=4097), -4), (dict(table_stride_b=-4), -2), (dict(lens_stride_h=-1), -2), (dict(k=_t(None)), -1), (dict(v=_t(None)), -1),
     (dict(k=_t(4104)), -4), (dict(v=_t(st=132)), -4), (dict(v=_t(st=64)), -2), (dict(k=_t(sb=-2048)), -2), (dict(v=_t(dt=0)), -3), (dict(k=_t(dt=3), v=_t(dt=3)), -3),
-    (dict(k=_t(sh=0)), -2), (dict(k_scale=4096, v_scale=4096), -3), (dict(k=_t(sb=1 << 41)), -2),
+    (dict(k=_t(sh=0)), -2), (dict(k_scale=4096, v_scale=4096), -3), (dict(k=_t(sb=1 << 41)), -2), (dict(k=_t(sb=0)), -2), (dict(v=_t(sb=0)), -2),
     (dict(dt=2, k_scale=None), -1), (dict(dt=2, v_scale=None), -1), (dict(dt=2, k_scale=4100), -4), (dict(dt=2, scale_stride_p=20), -4),
     (dict(dt=2, scale_stride_h=-8), -2), (dict(dt=2, k=_t(dt=2, st=136)), -4),
 ]
