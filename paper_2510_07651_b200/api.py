@@ -455,7 +455,8 @@ def evict_to_pages(q, k, v, cache: PagedCache, *, budget, seq_lens=None, variant
                    pool_kernel=1, causal=True, path="auto", safeguard=None):
     """The prefill hot path into pages: score -> pool/select -> the kept rows of k, v, quantised if need be, into the lists of `cache`, which
     become the whole lists: cache.lens is set.  With `safeguard` the budgets are head-adaptive and cache.lens is int32
-    [B,Hkv], contiguous (a head may keep as many tokens as its list's pages hold).  Returns (idx, scores)."""
+    [B,Hkv], contiguous (a head may keep as many tokens as its list's pages hold).  A sequence that the selection cannot serve (shorter than
+    the budget, or a head that would keep more than its list holds: rows of -1 in idx) leaves empty lists.  Returns (idx, scores)."""
     n_recent = q.shape[2] if n_recent is None else n_recent
     scores = obc_score(q, k, v, seq_lens=seq_lens, causal=causal, variants=(variant,), path=path)
     room = cache.table.shape[-1] * cache.k.shape[2]
@@ -464,11 +465,14 @@ def evict_to_pages(q, k, v, cache: PagedCache, *, budget, seq_lens=None, variant
             raise ValueError("the lists' pages do not hold the budget")
         idx = obc_select(scores[0], budget=budget, seq_lens=seq_lens, n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel)
         cache.lens.fill_(budget)
+        if seq_lens is not None:
+            cache.lens.mul_((seq_lens >= budget).view(-1, *[1] * (cache.lens.dim() - 1)))
         obc_paged_write(cache, k, v, idx=idx)
     else:
         if cache.lens.dim() != 2 or not cache.lens.is_contiguous() or (cache.table.dim() != 3 and cache.k.shape[1] > 1):
             raise ValueError("head-adaptive budgets need a list per head: lens [B,Hkv], table [B,Hkv,max_pages]")
         idx, _ = obc_select_adaptive(scores[0], budget=budget, safeguard=safeguard, idx_stride=min(room, k.shape[2]), seq_lens=seq_lens,
                                      n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel, counts=cache.lens)
+        cache.lens.clamp_(min=0)
         obc_paged_write(cache, k, v, new_lens=cache.lens, idx=idx)
     return idx, scores

@@ -344,6 +344,13 @@ bool on_device(const PagesArg& g, std::initializer_list<const Tensor*> ts) {
         if (t->defined() && t->device() != g.k->device()) return bad("all tensors must be on the pages' device");
     return true;
 }
+bool fits_32(std::initializer_list<const Tensor*> ts) {
+    for (const Tensor* t : ts)
+        if (t->defined())
+            for (const int64_t n : t->sizes())
+                if (n > 0x7fffffff) return bad("extents must fit 32 bits");
+    return true;
+}
 void* stream_of(const PagesArg& g) { return c10::cuda::getCurrentCUDAStream(g.k->device().index()).stream(); }
 
 // paged_write(k, v, table, lens, k_scale, v_scale, new_k, new_v, new_lens, idx) -> None
@@ -354,7 +361,7 @@ PyObject* n_paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor *nk, *nv, *lens, *idx;
     obc_tensor tk, tv;
     if (!pages_arg(a, &g) || !view4_arg(a[6], &nk, &tk) || !view4_arg(a[7], &nv, &tv) || !tensor_arg(a[8], &lens, true) || !tensor_arg(a[9], &idx, true) ||
-        !on_device(g, {nk, nv, lens, idx})) return nullptr;
+        !on_device(g, {nk, nv, lens, idx}) || !fits_32({nk, idx})) return nullptr;
     const int64_t B = g.c.batch, H = g.c.n_kv_heads;
     if (nk->size(0) != B || nk->size(1) != H || nk->size(3) != g.k->size(3) || nv->sizes() != nk->sizes()) { bad("k and v must be [batch, heads, tokens, head_dim] like the lists"); return nullptr; }
     if (lens->defined() && (lens->scalar_type() != at::kInt || (lens->dim() == 1 ? lens->size(0) != B : lens->dim() != 2 || lens->size(0) != B || lens->size(1) != H))) {
@@ -396,7 +403,7 @@ PyObject* n_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
         v_out = at::empty_like(k_out);
     }
     obc_tensor tk, tv;
-    if (!view4(k_out, &tk) || !view4(v_out, &tv)) return nullptr;
+    if (!view4(k_out, &tk) || !view4(v_out, &tv) || !fits_32({&k_out})) return nullptr;
     if (k_out.size(0) != g.c.batch || k_out.size(1) != g.c.n_kv_heads || k_out.size(3) != g.k->size(3) || v_out.sizes() != k_out.sizes()) {
         bad("k_out and v_out must be [batch, heads, tokens, head_dim] like the lists");
         return nullptr;
@@ -417,7 +424,7 @@ PyObject* n_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor *q, *q_lens, *o_in, *lse_in, *ws_in;
     obc_tensor tq, to;
     if (!pages_arg(a, &g) || !view4_arg(a[6], &q, &tq) || !tensor_arg(a[7], &q_lens, true) || !tensor_arg(a[10], &o_in, true) ||
-        !tensor_arg(a[11], &lse_in, true) || !tensor_arg(a[12], &ws_in, true) || !on_device(g, {q, q_lens, o_in, lse_in, ws_in})) return nullptr;
+        !tensor_arg(a[11], &lse_in, true) || !tensor_arg(a[12], &ws_in, true) || !on_device(g, {q, q_lens, o_in, lse_in, ws_in}) || !fits_32({q})) return nullptr;
     const double scale = PyFloat_AsDouble(a[8]);
     const long causal = as_long(a[9]);
     if (PyErr_Occurred()) return nullptr;

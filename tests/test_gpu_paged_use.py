@@ -119,6 +119,38 @@ def test_evict_to_pages(pages, safeguard):
                 assert ((got[b, h, :n].double() - rows).abs() <= tol).all() and (got[b, h, n:] == 0).all()
 
 
+@pytest.mark.parametrize("lens_dims", [1, 2])
+@pytest.mark.parametrize("safeguard", [None, 0.2])
+def test_evict_to_pages_of_sequences_shorter_than_the_budget(safeguard, lens_dims):
+    """Nothing is selected from such a sequence, so its lists are empty, whatever their pages held before; the others are as if alone."""
+    if safeguard is not None and lens_dims == 1:
+        pytest.skip("head-adaptive budgets have a length per head")
+    B, Hq, H, N, W, P, budget = 3, 8, 4, 300, 16, 16, 96
+    q, k, v = _rand((B, Hq, W, D), 1), _rand((B, H, N, D), 2), _rand((B, H, N, D), 3)
+    seq_lens = torch.tensor([300, 95, 96], dtype=torch.int32, device="cuda")
+    per = 19
+    pool = _pool(B * H * per, 1, P, "bf16")
+    pool[0].fill_(7.0); pool[1].fill_(7.0)
+    table = torch.arange(B * H * per, dtype=torch.int32, device="cuda").view(B, H, per)
+    lens = torch.zeros((B, H) if lens_dims == 2 else (B,), dtype=torch.int32, device="cuda")
+    cache = api.PagedCache(pool[0], pool[1], table, lens)
+    idx, _ = api.evict_to_pages(q, k, v, cache, budget=budget, seq_lens=seq_lens, safeguard=safeguard)
+    got = cache.lens.view(B, -1)
+    assert (idx[1] == -1).all() and (got[1] == 0).all()
+    if safeguard is None:
+        assert (got[0] == budget).all() and (got[2] == budget).all()
+    else:
+        assert int(got[0].sum()) == H * budget and int(got[2].sum()) == H * budget
+    o, lse = api.obc_paged_attention(q[:, :, :1].contiguous(), cache)
+    assert (o[1] == 0).all() and (lse[1] == -math.inf).all()
+    assert torch.isfinite(lse[0]).all() and torch.isfinite(lse[2]).all()
+    kd, _ = api.obc_paged_read(cache, n_tokens=per * P)
+    for b in (0, 2):
+        for h in range(H):
+            n = int(got[b, h if lens_dims == 2 else 0])
+            assert torch.equal(kd[b, h, :n], k[b, h][idx[b, h, :n].long()])
+
+
 def test_evict_to_pages_refuses_what_the_lists_cannot_hold():
     q, k = _rand((1, 4, 8, D), 1), _rand((1, 2, 100, D), 2)
     cache = api.PagedCache(*_pool(4, 2, 16, "bf16")[:2], torch.arange(2, dtype=torch.int32, device="cuda").view(1, 2), torch.zeros(1, dtype=torch.int32, device="cuda"))
@@ -239,3 +271,14 @@ def test_refused_on_the_gpu():
         api.obc_paged_write(L.cache, q[:, :2], q[:, :2], idx=torch.zeros((1, 2, 4), dtype=torch.int64, device="cuda"))
     with pytest.raises(ValueError, match="new_lens"):
         api.obc_paged_write(L.cache, q[:, :2], q[:, :2], new_lens=torch.zeros(3, dtype=torch.int32, device="cuda"))
+
+
+def test_extents_beyond_32_bits_are_refused():
+    L = Lists([70], 2, 16, "bf16", seed=2)
+    long = _rand((1, 2, 1, D), 1).expand(-1, -1, (1 << 32) + 1, -1)
+    with pytest.raises(ValueError, match="32 bits"):
+        api.obc_paged_attention(long, L.cache)
+    with pytest.raises(ValueError, match="32 bits"):
+        api.obc_paged_write(L.cache, long, long)
+    with pytest.raises(ValueError, match="32 bits"):
+        api.obc_paged_read(L.cache, k_out=long, v_out=long)
