@@ -2,17 +2,20 @@
 //
 // A CTA works on 256 query rows of a list, 128 per softmax warpgroup, one row per thread.  For tile i of 128 tokens and warpgroup w:
 //     S_w  = Q_w K_i^T                       accumulator in TMEM
-//     P_w  = 2^(S_w scale log2 e - m_w)      registers -> bf16 -> TMEM, over S_w's first 64 columns
-//     O_w += P_w V_i                         A operand from TMEM, V as MN-major B
-// While one warpgroup is at its exponentials the MMAs of the other run; a K or V tile is fetched once for both.  m_w only moves when a
-// tile's maximum exceeds it by more than 2^8, so that O_w is rescaled (in TMEM, by the thread that owns the row) a few times per
-// list.  The MMAs of a warpgroup are issued by one thread and execute in order: S_w(i+1) cannot overwrite P_w(i) before P_w V(i) has read it, and the
-// commit behind S_w(i+1) covers P_w V(i).
+//     P_w  = 2^(S_w scale log2 e - m_w)      registers -> bf16 -> shared memory (8-bit pages: TMEM, over S_w's first columns)
+//     O_w += P_w V_i                         V as MN-major B
+// A K or V tile is fetched once for both warpgroups.  m_w only moves when a tile's maximum exceeds it by more than 2^8, so that O_w is
+// rescaled (in TMEM, by the thread that owns the row) a few times per list.
+// With P in shared memory S_w(i+1) is formed while P_w(i) is still at work (S_w is free as soon as its values are in registers), so that a
+// warpgroup finds its next logits ready: 512 rows over 16384 tokens, 32 heads on 8, 137 -> 130 us; a 4096-token prompt 163 -> 157 us; the last 512 of 131072 tokens
+// 913 -> 865 us.  It takes 64 KB, which leaves the ring three operands of 32 KB.  8-bit pages need raw tiles beside that ring and would be left with two: there P
+// stays in TMEM, the MMAs of a warpgroup execute in order (S_w(i+1) cannot overwrite P_w(i) before P_w V(i) has read it), and those of one
+// run while the other is at its exponentials.
 //
-//   warp 0       producer: pages -> ring of 32 KB operands (K and V tiles in turn); 8-bit pages -> ring of raw tiles and their scales
+//   warps 0, 2   producers of K and of V: pages -> ring of 32 KB operands; 8-bit pages -> a raw tile each and its scales.  In V tiles at a list's end (16 bits)
+//                rows behind it become zeros; rows that are not finite and that not every query sees become zeros, too, and are named to the softmax warps,
+//                which add them by hand where they are seen
 //   warps 1, 3   MMA issuers, one for each softmax warpgroup (one thread for both was what set the pace)
-//   warp 2       V tiles at a list's end: rows behind it become zeros, rows that are not finite and that not
-//                every query sees become zeros, too, and are named to the softmax warps, which add them by hand where they are seen
 //   warps 4-11   softmax, two warpgroups; each fetches its Q
 //   warps 12-15  (8-bit pages) codes -> bf16 tiles, the scale multiplied in exactly; and what warp 2 does for V tiles
 // TMEM columns: S_0 [0,128)  S_1 [128,256)  O_0 [256,384)  O_1 [384,512)
@@ -27,18 +30,23 @@ constexpr int kChunkRows = 256;
 
 template <bool E4M3> struct ChunkLayout {
     static constexpr int kThreads = E4M3 ? 512 : 384;
-    static constexpr int kSlots = E4M3 ? 4 : 5;                                        // bf16 operands of 32 KB
+    static constexpr bool kPS = !E4M3;                                              // P in shared memory
+    // quarters of a tile's exponentials before the other warpgroup's turn.  With P in TMEM all: then the MMAs of one run beside the exponentials of the other.  Else half
+    // of them: one warp alone does not keep the unit busy (512 rows over 16384 tokens: 136 us with all, 133, 125, 126 with 1, 2, 3; without turns 187)
+    static constexpr int kTurn = kPS ? 2 : 4;
+    static constexpr int kSlots = (E4M3 ? 4 : 5) - (kPS ? 2 : 0);                      // bf16 operands of 32 KB
     static constexpr int kRaw = E4M3 ? 2 : 0;                                          // raw operands of 16 KB
-    static constexpr uint32_t kQ = 0, kRing = 2 * kOperandBytes, kRawAt = kRing + kSlots * kOperandBytes;
+    static constexpr uint32_t kQ = 0, kP = 2 * kOperandBytes, kRing = (kPS ? 4 : 2) * kOperandBytes, kRawAt = kRing + kSlots * kOperandBytes;
     static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
     static constexpr uint32_t kBad = kScales + kRaw * 128u;                            // [slot][4] words: tokens to be added by hand
     static constexpr uint32_t kBars = kBad + kSlots * 16u;
-    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PFULL = SFULL + 2, TURN = PFULL + 2, ODONE = TURN + 8, RAWFULL = ODONE + 2,
+    enum { FULL = 0, EMPTY = kSlots, EDGE = 2 * kSlots, QFULL = 3 * kSlots, SFULL = QFULL + 2, PFULL = SFULL + 2, TURN = PFULL + 2, ODONE = TURN + 8, SFREE = ODONE + 2, RAWFULL = SFREE + 2,
            RAWEMPTY = RAWFULL + 2, NBARS = RAWEMPTY + 2 };
     static constexpr uint32_t kTmem = kBars + NBARS * 8u;
     static constexpr uint32_t kSmem = kTmem + 16 + 1024;
     // registers: softmax warpgroups against the others, out of what the launch gives all threads
     static constexpr int kSoftRegs = E4M3 ? 184 : 208, kOtherRegs = E4M3 ? 72 : 88;
+    static_assert(!kPS || kSlots >= 3, "places between two operands of a producer");
     static_assert(256 * kSoftRegs + (kThreads - 256) * kOtherRegs <= kThreads * (E4M3 ? 128 : 168), "registers");
 };
 
@@ -102,7 +110,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         prefetch_tmap(&map_k); prefetch_tmap(&map_v);
         for (int i = 0; i < NS; ++i) { mbar_init(bar(L::FULL + i), E4M3 ? 4 : 1); mbar_init(bar(L::EMPTY + i), 2); mbar_init(bar(L::EDGE + i), 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1);
+            mbar_init(bar(L::QFULL + i), 128); mbar_init(bar(L::SFULL + i), 1); mbar_init(bar(L::PFULL + i), 4); mbar_init(bar(L::ODONE + i), 1); mbar_init(bar(L::SFREE + i), 4);
             mbar_init(bar(L::RAWFULL + i), 33); mbar_init(bar(L::RAWEMPTY + i), 4);
         }
         for (int i = 0; i < 8; ++i) mbar_init(bar(L::TURN + i), 1);
@@ -132,52 +140,93 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         return false;
     };
     // V tiles that reach behind what every row sees pass through warp 2 before anyone else may read them (16-bit pages): their copies complete
-    // on the slot's EDGE barrier, whose parity warp 2 keeps (a bit per slot), and warp 2 arrives on FULL in their stead.
+    // on the slot's EDGE barrier, whose parity warp 2 keeps (a bit per slot), and warp 2 arrives on FULL in their stead.  (The two producers' operands share the
+    // ring.  A producer's next operand is at most three places behind its last, no more than the ring has slots, so that its wait for a slot's round
+    // cannot be taken for one two rounds earlier.)
+    // Operands are numbered in the order in which they are fetched and used.  Of a segment's n tiles, of which tile 0 is the run's tile `base`: K(0) V(0) K(1)
+    // V(1) .., or with P in shared memory, where S is formed a tile ahead of P V, K(0) K(1) V(0) K(2) V(1) .. K(n-1) V(n-2) V(n-1).
+    auto k_number = [](uint32_t base, int i) { return 2 * base + (L::kPS && i > 0 ? 2 * i - 1 : 2 * i); };
+    auto v_number = [](uint32_t base, int i, int n) { return 2 * base + (L::kPS && i + 1 < n ? 2 * i + 2 : 2 * i + 1); };
     auto is_edge = [&](const ChunkSeg& c, int t0) { return t0 + kTokTile > c.first_masked; };
 
     if (warp < 4) {
         fewer_registers<L::kOtherRegs>();
-        if (warp == 0) {
-            // ===================================== producer =====================================
+        if ((warp & 1) == 0) {
+            // ===================================== producers ====================================
+            // (A copy takes a warp some 90 cycles to issue, one lane after the other: with pages of 16 tokens an operand is 16 of them.)
+            const int op = warp >> 1;                               // K or V
+            const CUtensorMap* map = op ? &map_v : &map_k;
             TileWalk<kChunkRows> walk(p, run, lane);
-            uint32_t n = 0;                                         // operands issued
+            uint32_t n = 0, base = 0, edges = 0;                    // tiles fetched, before this segment; EDGE parities, a bit per slot
+            uint32_t recent[NS] = {};                               // the last operands
             while (walk.more && !fail_site) {
                 const int pg = walk.page(), h = walk.cur.m.h, slot = walk.slot, hh = p.one_head ? 0 : h, at = lane << (p.box_shift + 7);
-                const bool edge = walk.tile * kTokTile + kTokTile > seen_by(p, walk.cur.m, 0);
-                for (int op = 0; op < 2; ++op, ++n) {
-                    const CUtensorMap* map = op ? &map_v : &map_k;
-                    if (E4M3) {
-                        const uint32_t st = n & 1, full = bar(L::RAWFULL + st);
-                        if (!all_wait(L::RAWEMPTY + st, (n >> 1) ^ 1u, __LINE__)) break;
-                        if (lane == 0) mbar_expect_tx(full, 16384);
-                        __syncwarp();
-                        if (lane < walk.boxes()) tma_load_4d(sbase + L::kRawAt + st * 16384u + at, map, full, 0, slot, hh, pg);
-                        const int t8 = (lane & 15) * 8, ps = __shfl_sync(0xffffffffu, pg, t8 >> p.box_shift);
-                        if (lane < 16) {
-                            const uint8_t* src = (op ? p.c.vs : p.c.ks) + (ps < 0 ? 0ll : ps * p.c.ss_p + h * p.c.ss_h + walk.slot8);
-                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(sbase + L::kScales + st * 128u + t8), "l"(src), "r"(ps < 0 ? 0 : 8) : "memory");
+                if (E4M3) {
+                    const uint32_t full = bar(L::RAWFULL + op);
+                    if (!all_wait(L::RAWEMPTY + op, n ^ 1u, __LINE__)) break;
+                    if (lane == 0) mbar_expect_tx(full, 16384);
+                    __syncwarp();
+                    if (lane < walk.boxes()) tma_load_4d(sbase + L::kRawAt + op * 16384u + at, map, full, 0, slot, hh, pg);
+                    const int t8 = (lane & 15) * 8, ps = __shfl_sync(0xffffffffu, pg, t8 >> p.box_shift);
+                    if (lane < 16) {
+                        const uint8_t* src = (op ? p.c.vs : p.c.ks) + (ps < 0 ? 0ll : ps * p.c.ss_p + h * p.c.ss_h + walk.slot8);
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(sbase + L::kScales + op * 128u + t8), "l"(src), "r"(ps < 0 ? 0 : 8) : "memory");
+                    }
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
+                } else {
+                    const int i = walk.tile - walk.cur.ta, t0 = walk.tile * kTokTile, len = walk.cur.m.len, masked = seen_by(p, walk.cur.m, 0);
+                    const bool edge = op && t0 + kTokTile > masked;
+                    const uint32_t k = op ? v_number(base, i, walk.cur.tb - walk.cur.ta) : k_number(base, i), st = k % NS, full = bar((edge ? L::EDGE : L::FULL) + st);
+                    if (!all_wait(L::EMPTY + st, (k / NS) ^ 1u, __LINE__)) break;
+#pragma unroll
+                    for (int j = 0; j < NS; ++j) recent[j] = j + 1 < NS ? recent[j + 1] : k;
+                    if (lane == 0) mbar_expect_tx(full, kOperandBytes);
+                    __syncwarp();
+                    if (lane < walk.boxes()) {
+                        const uint32_t d = sbase + L::kRing + st * kOperandBytes + at;
+                        tma_load_4d(d, map, full, 0, slot, hh, pg);
+                        tma_load_4d(d + kHalfBytes, map, full, 64, slot, hh, pg);
+                    }
+                    // rows behind the list become zeros; so do rows that are not finite and that not every query sees, which are named to the softmax warps
+                    if (edge) {
+                        if (!all_wait(L::EDGE + st, edges >> st, __LINE__)) break;
+                        edges ^= 1u << st;
+                        uint8_t* tile = smem + L::kRing + st * kOperandBytes;
+#pragma unroll 1
+                        for (int j = 0; j < 4; ++j) {
+                            const int row = j * 32 + lane, t = t0 + row;
+                            bool odd = false;
+                            if (t >= masked && t < len) {
+#pragma unroll
+                                for (int ch = 0; ch < 16; ++ch) {
+                                    const uint4 u = *reinterpret_cast<const uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
+                                    odd |= not_finite(u.x) || not_finite(u.y) || not_finite(u.z) || not_finite(u.w);
+                                }
+                            }
+                            if (odd || t >= len) {
+#pragma unroll
+                                for (int ch = 0; ch < 16; ++ch)
+                                    *reinterpret_cast<uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            const uint32_t word = __ballot_sync(0xffffffffu, odd);
+                            if (lane == 0) bad_words[st * 4 + j] = word;
                         }
-                        asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(full) : "memory");
-                    } else {
-                        const uint32_t st = n % NS, full = bar((op && edge ? L::EDGE : L::FULL) + st);
-                        if (!all_wait(L::EMPTY + st, (n / NS) ^ 1u, __LINE__)) break;
-                        if (lane == 0) mbar_expect_tx(full, kOperandBytes);
+                        fence_async_smem();
                         __syncwarp();
-                        if (lane < walk.boxes()) {
-                            const uint32_t d = sbase + L::kRing + st * kOperandBytes + at;
-                            tma_load_4d(d, map, full, 0, slot, hh, pg);
-                            tma_load_4d(d + kHalfBytes, map, full, 64, slot, hh, pg);
-                        }
+                        if (lane == 0) mbar_arrive(bar(L::FULL + st));
                     }
                 }
-                if (n == 2) walk.look_ahead();
+                if (n++ == 0) walk.look_ahead();
+                if (walk.tile + 1 == walk.cur.tb) base = n;
                 walk.advance();
             }
-            // no copy may be under way when the CTA leaves
-            const uint32_t ring = E4M3 ? 2u : (uint32_t)NS;
-            for (uint32_t back = 0; back < ring && back < n; ++back) {
-                const uint32_t k = n - 1 - back;
-                (void)mbar_wait(bar((E4M3 ? (int)L::RAWFULL : (int)L::FULL) + k % ring), (k / ring) & 1u);
+            // no copy may be under way when the CTA leaves: the last operand of every slot
+            if (E4M3) {
+                if (n > 0) (void)mbar_wait(bar(L::RAWFULL + op), (n - 1) & 1u);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NS; ++j)
+                    if (j + n >= NS && recent[j] + NS >= 2 * n) (void)mbar_wait(bar(L::FULL + recent[j] % NS), (recent[j] / NS) & 1u);
             }
         } else if (warp & 1) {
             // ===================================== MMA issuers ======================================
@@ -187,10 +236,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const bool leader = elect_one();
             const uint32_t idesc_s = idesc_bf16(kTokTile);
             const uint32_t idesc_pv = idesc_bf16(kD) | (1u << 16);               // B operand (V) is MN-major
-            const uint32_t aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes), tS = tmem + w * 128u, tO = tmem + 256u + w * 128u;
+            const uint32_t aq = desc_lo_k(sbase + L::kQ + w * kOperandBytes), ap = desc_lo_k(sbase + L::kP + w * kOperandBytes), tS = tmem + w * 128u, tO = tmem + 256u + w * 128u;
             Segments<kChunkRows> seg(p, run);
-            uint32_t op = 0, slot = 0, phase = 0, np = 0, nq = 0;                // operand, its slot and round; P tiles taken; Q tiles taken
-            auto next_op = [&]() { ++op; if (++slot == NS) { slot = 0; phase ^= 1u; } };
+            uint32_t slot = 0, phase = 0, ns = 0, np = 0, nq = 0;                // the operand's slot and round; S tiles begun, P and Q tiles taken
+            auto next_op = [&]() { if (++slot == NS) { slot = 0; phase ^= 1u; } };
             while (seg.next()) {
                 const ChunkSeg c = chunk_seg(p, seg);
                 const int n = uniform(c.n), cnt = uniform(c.cnt(w));
@@ -198,6 +247,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 auto step_s = [&](int i) -> bool {
                     if (!all_wait(L::FULL + slot, phase, __LINE__)) return false;
                     if (i < cnt) {
+                        if (L::kPS && ns++ > 0 && !all_wait(L::SFREE + w, ns, __LINE__)) return false;
                         tc_fence_after();
                         if (leader) {
                             const uint32_t ak = desc_lo_k(sbase + L::kRing + slot * kOperandBytes);
@@ -217,6 +267,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 if (cnt > 0 && !all_wait(L::QFULL + w, nq++, __LINE__)) break;
                 if (!step_s(0)) break;
                 for (int i = 0; i < n; ++i) {
+                    if (L::kPS && i + 1 < n && !step_s(i + 1)) break;
                     if (!all_wait(L::FULL + slot, phase, __LINE__)) break;
                     if (i < cnt) {
                         const uint32_t av = desc_lo_mn(sbase + L::kRing + slot * kOperandBytes);
@@ -225,63 +276,22 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         if (leader) {
 #pragma unroll
                             for (int ks = 0; ks < 8; ++ks)               // steps of K = 16 tokens (2048 bytes of V each)
-                                tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
+                                if constexpr (L::kPS) tc_mma(tO, desc_make(ap + desc_kstep(ks, kHalfBytes)), desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
+                                else tc_mma_ts(tO, tS + ks * 8, desc_make(av + ks * (2048 >> 4)), idesc_pv, 1u);
                         }
                         ++np;
                         if (leader) {
                             tc_commit(bar(L::EMPTY + slot));
-                            if (i == cnt - 1) tc_commit(bar(L::ODONE + w));
+                            if (L::kPS || i == cnt - 1) tc_commit(bar(L::ODONE + w));
                         }
                     } else if (leader) {
                         mbar_arrive(bar(L::EMPTY + slot));
                     }
                     __syncwarp();
                     next_op();
-                    if (i + 1 < n && !step_s(i + 1)) break;
+                    if (!L::kPS && i + 1 < n && !step_s(i + 1)) break;
                 }
                 if (fail_site) break;
-            }
-        } else {
-            // ======================= V tiles at the end of what is seen =======================
-            if (!E4M3) {
-                Segments<kChunkRows> seg(p, run);
-                uint32_t base = 0, edges = 0;
-                while (!fail_site && seg.next()) {
-                    const Item& m = seg.m;
-                    const ChunkSeg c = chunk_seg(p, seg);
-                    for (int i = 0; i < c.n; ++i) {
-                        const int t0 = (seg.ta + i) * kTokTile;
-                        if (!is_edge(c, t0)) continue;
-                        const uint32_t op = 2 * (base + i) + 1;
-                        const int vs = op % NS;
-                        if (!all_wait(L::EDGE + vs, edges >> vs, __LINE__)) break;
-                        edges ^= 1u << vs;
-                        uint8_t* tile = smem + L::kRing + vs * kOperandBytes;
-#pragma unroll 1
-                        for (int j = 0; j < 4; ++j) {
-                            const int row = j * 32 + lane, t = t0 + row;
-                            bool odd = false;
-                            if (t >= c.first_masked && t < m.len) {
-#pragma unroll
-                                for (int ch = 0; ch < 16; ++ch) {
-                                    const uint4 u = *reinterpret_cast<const uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4));
-                                    odd |= not_finite(u.x) || not_finite(u.y) || not_finite(u.z) || not_finite(u.w);
-                                }
-                            }
-                            if (odd || t >= m.len) {
-#pragma unroll
-                                for (int ch = 0; ch < 16; ++ch)
-                                    *reinterpret_cast<uint4*>(tile + (ch >> 3) * kHalfBytes + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-                            }
-                            const uint32_t word = __ballot_sync(0xffffffffu, odd);
-                            if (lane == 0) bad_words[vs * 4 + j] = word;
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bar(L::FULL + vs));
-                    }
-                    base += c.n;
-                }
             }
         }
     } else if (warp < 12) {
@@ -349,12 +359,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     if (!all_wait(L::SFULL + w, ns, __LINE__)) break;
                     ++ns;
                     tc_fence_after();
+
                     uint32_t s[128];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) tc_ld32(tS + q * 32, s + q * 32);
                     tc_wait_ld32(s);
 #pragma unroll
                     for (int q = 1; q < 4; ++q) tc_wait_ld32(s + q * 32);
+                    if (L::kPS) {                                   // S is read: the next one may be formed
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(L::SFREE + w));
+                    }
                     const int nvis = seen - t0;                     // columns j < nvis are seen
                     if (edge && __any_sync(0xffffffffu, nvis < kTokTile)) {
 #pragma unroll
@@ -368,6 +384,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         for (int j = 8; j < 128; j += 8) t4[q] = fmax3(t4[q], __uint_as_float(s[j + q]), __uint_as_float(s[j + q + 4]));
                     }
                     const float mt = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * p.sl2;
+                    // The two warps of an SM sub-partition take turns at the exponentials, one per warpgroup: left alone they run side by side, and then
+                    // wait side by side for their MMAs.  (Warpgroup 0 begins; its turn k follows turn k - 1 of warpgroup 1.)
+                    if (i < both) {
+                        if ((w == 1 || turns > 0) && !all_wait(L::TURN + 4 * w + lane_grp, w ? turns : turns - 1u, __LINE__)) break;
+                        ++turns;
+                    }
+                    if (L::kPS && no > 0) {                         // P V of the tile before
+                        if (!all_wait(L::ODONE + w, no - 1u, __LINE__)) break;
+                        tc_fence_after();
+                    }
+                    if (L::kPS) ++no;
                     const bool need = mt > m_used + 8.f;            // also true for the first tile that is seen
                     if (__any_sync(0xffffffffu, need)) {
                         const float factor = need ? fast_exp2(m_used - mt) : 1.f;
@@ -390,15 +417,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     const float m_eff = m_used == -INFINITY ? 0.f : m_used;
                     const float2 negm = make_float2(-m_eff, -m_eff);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    // The two warps of an SM sub-partition take turns at the exponentials, one per warpgroup: left alone they run side by side, and then
-                    // wait side by side for their MMAs.  (Warpgroup 0 begins; its turn k follows turn k - 1 of warpgroup 1.)
-                    if (i < both) {
-                        if ((w == 1 || turns > 0) && !all_wait(L::TURN + 4 * w + lane_grp, w ? turns : turns - 1u, __LINE__)) break;
-                        ++turns;
-                    }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t pk[16];
+                        if (q == L::kTurn && i < both && lane == 0) mbar_arrive(bar(L::TURN + 4 * (w ^ 1) + lane_grp));
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             float2 x = make_float2(__uint_as_float(s[q * 32 + j]), __uint_as_float(s[q * 32 + j + 1]));
@@ -407,13 +429,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             sum[(j >> 1) & 1] = __fadd2_rn(sum[(j >> 1) & 1], ex);
                             pk[j >> 1] = pack_bf16x2(ex.x, ex.y);
                         }
-                        tc_st16(tS + q * 16, pk);
+                        if constexpr (L::kPS) {
+                            uint8_t* d = smem + L::kP + w * kOperandBytes + (q >> 1) * kHalfBytes + row * 128;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                *reinterpret_cast<uint4*>(d + ((((q & 1) * 4 + x) ^ (row & 7)) << 4)) = make_uint4(pk[4 * x], pk[4 * x + 1], pk[4 * x + 2], pk[4 * x + 3]);
+                        } else {
+                            tc_st16(tS + q * 16, pk);
+                        }
                     }
-                    if (i < both && lane == 0) mbar_arrive(bar(L::TURN + 4 * (w ^ 1) + lane_grp));
+                    if (L::kTurn == 4 && i < both && lane == 0) mbar_arrive(bar(L::TURN + 4 * (w ^ 1) + lane_grp));
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                     tc_wait_st();
                     if (edge) {                                     // rows of V that are added by hand
-                        const uint32_t vop = 2 * (base + i) + 1, vs = vop % NS;
+                        const uint32_t vop = v_number(base, i, c.n), vs = vop % NS;
                         if (!all_wait(L::FULL + vs, vop / NS, __LINE__)) break;
 #pragma unroll 1
                         for (int b = 0; b < 4; ++b) {
@@ -421,9 +450,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             while (word) {
                                 const int j = b * 32 + __ffs(word) - 1;
                                 word &= word - 1;
-                                uint32_t two;
-                                tc_ld1(tS + (j >> 1), two);
-                                const float wt = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+                                float wt;
+                                if constexpr (L::kPS) {
+                                    wt = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(smem + L::kP + w * kOperandBytes + (j >> 6) * kHalfBytes + row * 128 + ((((j >> 3) & 7) ^ (row & 7)) << 4) + (j & 7) * 2));
+                                } else {
+                                    uint32_t two;
+                                    tc_ld1(tS + (j >> 1), two);
+                                    wt = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
+                                }
                                 const int t = t0 + j, page = E4M3 ? -1 : p.c.page_of(m.b, m.h, t);
 #pragma unroll 1
                                 for (int q = 0; q < 8; ++q) {
@@ -444,9 +478,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             }
                         }
                     }
+                    if (L::kPS) fence_async_smem();
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::PFULL + w));
+
                 }
             }
             base += c.n;
@@ -454,8 +490,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             if (next_q) ask_q(seg.m);
             // ---- the segment's result ----
             if (cnt > 0) {
-                if (!all_wait(L::ODONE + w, no, __LINE__)) break;
-                ++no;
+                if (!all_wait(L::ODONE + w, L::kPS ? no - 1u : no, __LINE__)) break;
+                if (!L::kPS) ++no;
                 tc_fence_after();
             }
             const float k = whole ? (l != 0.f ? 1.f / l : 0.f) : 1.f;
