@@ -4,7 +4,7 @@
 // warp-level MMAs with the tokens on the M side, so that the (at most 8 per step) rows lie on N and nothing is padded to more:
 //     S^T = K q^T      16 tokens x 8 rows, 8 steps of 16 channels
 //     O^T += V^T P^T   16 channels x 8 rows, 8 tiles, one step of 16 tokens; P^T is S^T's accumulator turned by movmatrix
-// A warp keeps (m, l, O) of its own tokens; they meet once per segment.  P enters as bf16(P) + bf16(P - bf16(P)), so that o is off by no
+// A warp keeps (m, l, O) of its own tokens; they meet once per segment.  P enters as two bf16 parts, so that o is off by no
 // more than its own rounding (the MMAs are nowhere near their limit here).  With up to 8 rows two CTAs share an SM, so that one's segment
 // beginnings and ends (q, the joining of its warps' results) hide behind the other's tiles: 256 lists of 4096 tokens in 8 bits 74 -> 65 us.
 // Tiles of 16-bit rows are halved for it (three stages of 64 tokens each).
@@ -84,6 +84,13 @@ __device__ __forceinline__ float q_fragments(uint32_t (&b)[8][2], const __nv_bfl
 #pragma unroll
         for (int j = 0; j < 2; ++j) b[ks][j] = pack_f16x2(__uint_as_float(b[ks][j] << 16) * f, __uint_as_float(b[ks][j] & 0xffff0000u) * f);
     return pow2i(-up);
+}
+// Two weights (0 or more) as bf16 pairs hi + lo, off by at most 2^-16 of themselves.  Both parts of a weight above 2^-110 are above 0 (hi is cut off below the weight), so that
+// an infinity of V times them stays one: with hi rounded to nearest, lo may be 0 or negative, and their sum NaN.
+__device__ __forceinline__ void split_weights(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const uint32_t u = max(__float_as_uint(x), 1u) - 1u, v = max(__float_as_uint(y), 1u) - 1u;
+    hi = __byte_perm(u, v, 0x7632);
+    lo = pack_bf16x2(x - __uint_as_float(u & 0xffff0000u), y - __uint_as_float(v & 0xffff0000u));
 }
 // an 8x8 tile of 16-bit values turned: the lane's pair (row lane / 4, columns 2 (lane % 4), + 1) becomes that of the transpose
 __device__ __forceinline__ uint32_t turned(uint32_t x) {
@@ -313,7 +320,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             if (E4M3) {
                                 ph[nt][j] = turned(pack_f16x2(e[nt][2 * j] * fv[j], e[nt][2 * j + 1] * fv[j]));
                             } else {
-                                split_bf16x2(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
+                                split_weights(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
                                 ph[nt][j] = turned(hi); pl[nt][j] = turned(lo);
                             }
                         }

@@ -232,6 +232,20 @@ def test_infinities_and_nan_reach_only_the_queries_that_see_them(pages, what):
     assert torch.isfinite(lse[:, :2]).all()
 
 
+@pytest.mark.parametrize("pages", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("what", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("T,Hq,H", [(1, 8, 2), (2, 4, 1), (4, 8, 2), (40, 4, 2)])
+def test_infinities_that_every_query_sees(pages, what, T, Hq, H):
+    """They reach every output of their channel as the formula has it (an infinity stays one, whatever its weight's parts), and no other."""
+    n = 700
+    g = torch.Generator().manual_seed(12)
+    k, v = torch.randn((1, H, n, D), generator=g), torch.randn((1, H, n, D), generator=g)
+    for t, ch in ((0, 3), (131, 64), (350, 127), (513, 5)):
+        v[0, :, t, ch] = what
+    k[0, :, 350] *= 4                                 # (among its list's largest weights, and smallest)
+    _attend(Lists([n], H, 16, pages, seed=2, k=k, v=v), Hq, T, weight_bits=(BITS if Hq // H * T <= 16 else CHUNK_BITS)[pages])
+
+
 def test_long_list_behind_32_bits():
     """A pool of more than 2^32 elements; the list's pages lie at both of its ends."""
     P, H = 128, 2
