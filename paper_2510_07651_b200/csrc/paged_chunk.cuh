@@ -359,7 +359,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     if (!all_wait(L::SFULL + w, ns, __LINE__)) break;
                     ++ns;
                     tc_fence_after();
-
                     uint32_t s[128];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) tc_ld32(tS + q * 32, s + q * 32);
@@ -399,7 +398,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     if (__any_sync(0xffffffffu, need)) {
                         const float factor = need ? fast_exp2(m_used - mt) : 1.f;
                         if (__any_sync(0xffffffffu, need && m_used != -INFINITY)) {
-                            // P V of this warpgroup's previous tile is complete (the commit that signalled S covers it)
+                            // P V of this warpgroup's previous tile is complete (waited for above, or covered by the commit that signalled S)
 #pragma unroll 1
                             for (int q = 0; q < 8; ++q) {
                                 uint32_t ov[16];

@@ -295,6 +295,16 @@ def test_chunks_of_a_padded_batch(pages):
 
 
 @pytest.mark.parametrize("pages", ["bf16", "e4m3"])
+@pytest.mark.parametrize("P", [16, 64])
+def test_many_short_lists_in_chunks(pages, P):
+    """More row tiles than CTAs, of one to four token tiles each, some without rows of the second warpgroup or any: every CTA goes through several lists."""
+    g = torch.Generator().manual_seed(P)
+    lens = torch.randint(1, 500, (24,), generator=g).tolist()
+    q_lens = torch.randint(0, 81, (24,), generator=g).tolist()
+    _attend(Lists(lens, 8, P, pages, seed=5), 32, 80, q_lens=q_lens, weight_bits=CHUNK_BITS[pages])
+
+
+@pytest.mark.parametrize("pages", ["bf16", "e4m3"])
 @pytest.mark.parametrize("Hq", [2, 8, 14, 32])
 def test_single_tokens_beside_chunks(pages, Hq):
     """Lists of few rows, of the most that the kernel for few takes (and one more), and of many in one call, long and short ones of each."""
