@@ -32,7 +32,8 @@ template <bool E4M3> struct ChunkLayout {
     static constexpr int kThreads = E4M3 ? 512 : 384;
     static constexpr bool kPS = !E4M3;                                              // P in shared memory
     // quarters of a tile's exponentials before the other warpgroup's turn.  With P in TMEM all: then the MMAs of one run beside the exponentials of the other.  Else half
-    // of them: one warp alone does not keep the unit busy (512 rows over 16384 tokens: 136 us with all, 133, 125, 126 with 1, 2, 3; without turns 187)
+    // of them: one warp alone does not keep the unit busy (512 rows over 16384 tokens: 136 us with all, 133, 125, 126
+    // with 1, 2, 3; the last 512 of 131072 tokens on another GPU: 930 us with all, 995 without turns)
     static constexpr int kTurn = kPS ? 2 : 4;
     static constexpr int kSlots = (E4M3 ? 4 : 5) - (kPS ? 2 : 0);                      // bf16 operands of 32 KB
     static constexpr int kRaw = E4M3 ? 2 : 0;                                          // raw operands of 16 KB
