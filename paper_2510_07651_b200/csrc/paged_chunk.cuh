@@ -35,7 +35,7 @@ template <bool E4M3> struct ChunkLayout {
     // of them: one warp alone does not keep the unit busy (512 rows over 16384 tokens: 136 us with all, 133, 125, 126
     // with 1, 2, 3; the last 512 of 131072 tokens on another GPU: 930 us with all, 995 without turns)
     static constexpr int kTurn = kPS ? 2 : 4;
-    static constexpr int kSlots = (E4M3 ? 4 : 5) - (kPS ? 2 : 0);                      // bf16 operands of 32 KB
+    static constexpr int kSlots = E4M3 ? 4 : 3;                                        // bf16 operands of 32 KB
     static constexpr int kRaw = E4M3 ? 2 : 0;                                          // raw operands of 16 KB
     static constexpr uint32_t kQ = 0, kP = 2 * kOperandBytes, kRing = (kPS ? 4 : 2) * kOperandBytes, kRawAt = kRing + kSlots * kOperandBytes;
     static constexpr uint32_t kScales = kRawAt + kRaw * 16384u;                        // [raw slot][128]
