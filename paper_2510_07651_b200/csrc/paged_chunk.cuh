@@ -141,9 +141,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         return false;
     };
     // V tiles that reach behind what every row sees pass through warp 2 before anyone else may read them (16-bit pages): their copies complete
-    // on the slot's EDGE barrier, whose parity warp 2 keeps (a bit per slot), and warp 2 arrives on FULL in their stead.  (The two producers' operands share the
-    // ring.  A producer's next operand is at most three places behind its last, no more than the ring has slots, so that its wait for a slot's round
-    // cannot be taken for one two rounds earlier.)
+    // on the slot's EDGE barrier, whose parity warp 2 keeps (a bit per slot), and warp 2 arrives on FULL in their stead.
+    // The two producers' operands share the ring, and a wait by parity passes for a slot that is two rounds behind, too.  That cannot be as long as each
+    // issuer releases operands in their order: a producer's next operand, number k, is at most three places (the ring's slots) behind its last, for which
+    // operand k - 6 or a later one was released, and so k - 6 itself, the one two rounds earlier in k's slot, was.  An operand that a warpgroup does
+    // not see is therefore released by a commit as well: a plain arrival would overtake the MMAs that still read the operands before it.
     // Operands are numbered in the order in which they are fetched and used.  Of a segment's n tiles, of which tile 0 is the run's tile `base`: K(0) V(0) K(1)
     // V(1) .., or with P in shared memory, where S is formed a tile ahead of P V, K(0) K(1) V(0) K(2) V(1) .. K(n-1) V(n-2) V(n-1).
     auto k_number = [](uint32_t base, int i) { return 2 * base + (L::kPS && i > 0 ? 2 * i - 1 : 2 * i); };
@@ -221,13 +223,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 if (walk.tile + 1 == walk.cur.tb) base = n;
                 walk.advance();
             }
-            // no copy may be under way when the CTA leaves: the last operand of every slot
+            // no copy may be under way when the CTA leaves, and no commit's arrival: the last operand of every slot
             if (E4M3) {
                 if (n > 0) (void)mbar_wait(bar(L::RAWFULL + op), (n - 1) & 1u);
             } else {
 #pragma unroll
                 for (int j = 0; j < NS; ++j)
-                    if (j + n >= NS && recent[j] + NS >= 2 * n) (void)mbar_wait(bar(L::FULL + recent[j] % NS), (recent[j] / NS) & 1u);
+                    if (j + n >= NS && recent[j] + NS >= 2 * n) {
+                        (void)mbar_wait(bar(L::FULL + recent[j] % NS), (recent[j] / NS) & 1u);
+                        if (!fail_site) (void)all_wait(L::EMPTY + recent[j] % NS, recent[j] / NS, __LINE__);
+                    }
             }
         } else if (warp & 1) {
             // ===================================== MMA issuers ======================================
@@ -259,7 +264,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             tc_commit(bar(L::EMPTY + slot));
                         }
                     } else if (leader) {
-                        mbar_arrive(bar(L::EMPTY + slot));
+                        tc_commit(bar(L::EMPTY + slot));
                     }
                     __syncwarp();
                     next_op();
@@ -286,7 +291,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                             if (L::kPS || i == cnt - 1) tc_commit(bar(L::ODONE + w));
                         }
                     } else if (leader) {
-                        mbar_arrive(bar(L::EMPTY + slot));
+                        tc_commit(bar(L::EMPTY + slot));
                     }
                     __syncwarp();
                     next_op();
@@ -582,6 +587,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 }
             }
         }
+        for (uint32_t k = n > NS ? n - NS : 0u; k < n && !fail_site; ++k) (void)all_wait(L::EMPTY + k % NS, k / NS, __LINE__);      // (no commit's arrival may be under way when the CTA leaves)
     }
     if (fail_site) atomicCAS(p.status, 0u, (unsigned)fail_site);
     tc_fence_before();
