@@ -14,8 +14,9 @@
 // taken in the order in which ldmatrix hands out their bytes (q is loaded in the same order), and the rows of an O^T tile are eight even and
 // eight odd channels.  q is scaled by a power of two per row, so that its largest value is near 2^14 (what falls below fp16's range is less
 // than 2^-38 of it).  The scale of a K row goes into its logit, that of a V row into its P, relative to a reference exponent that O carries: P is
-// fp16 then, off by at most 2^-11 of itself.  Where the V rows of 16 tokens lie further apart than fp16's range allows they are taken by
-// classes of exponents.
+// fp16 then, off by at most 2^-11 of itself.  Where one of 16 tokens' weights (V's scale included) is above 0 and below 2^-14, where fp16 has fewer bits,
+// they are taken by classes of exponents, each scaled into fp16's normal range and added to O from accumulators of its own: beside a first token that
+// takes nearly all of the weight, with a row of V near 0, o consists of such weights.
 #pragma once
 #include "paged_common.cuh"
 #include "tc_ptx.cuh"
@@ -52,6 +53,8 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// a weight above 0 that fp16 holds with fewer than its 11 bits, or not at all
+__device__ __forceinline__ bool below_f16(float x) { return __float_as_uint(x) - 1u < 0x387fffffu; }
 // 2^e for whole e (0 and infinity beyond fp32's exponents)
 __device__ __forceinline__ float pow2i(int e) { return e < -126 ? 0.f : e > 127 ? INFINITY : __uint_as_float((uint32_t)(e + 127) << 23); }
 // a row's scale from its byte
@@ -264,11 +267,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         const uint8_t* sc = smem + L::kScales + s_at * 256 + tok0 + g;
                         fk[0] = scale_of(sc[0]); fk[1] = scale_of(sc[8]);
                         ev[0] = sc[128]; ev[1] = sc[136];
-                        // exponents of the V rows that the list has: highest (of the finite ones) and lowest
+                        // highest exponent of the V rows that the list has (of the finite ones)
                         const bool in0 = t0 + g < m.len, in1 = t0 + g + 8 < m.len;
                         const int hi = __reduce_max_sync(0xffffffffu, max(in0 && ev[0] < 255 ? ev[0] : 0, in1 && ev[1] < 255 ? ev[1] : 0));
-                        const int lo = __reduce_min_sync(0xffffffffu, min(in0 ? ev[0] : 255, in1 ? ev[1] : 255));
-                        const bool nan = __any_sync(0xffffffffu, (in0 && ev[0] == 255) || (in1 && ev[1] == 255));
                         if (e_ref < 0 || hi > e_ref + 4) {          // O follows: P stays below 2^12
                             const float f = e_ref < 0 ? 0.f : pow2i(e_ref - hi);
 #pragma unroll
@@ -277,7 +278,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                                 for (int j = 0; j < 8; ++j) { o[nt][j][0] *= f; o[nt][j][1] *= f; o[nt][j][2] *= f; o[nt][j][3] *= f; }
                             e_ref = hi;
                         }
-                        classes = nan || lo < e_ref - 8;
+                        classes = (in0 && ev[0] == 255) || (in1 && ev[1] == 255);
                         fv[0] = in0 ? pow2i(ev[0] - e_ref) : 0.f; fv[1] = in1 ? pow2i(ev[1] - e_ref) : 0.f;
                     }
                     uint32_t ph[NT][2], pl[NT][2];                  // P^T as B operands: high and low parts
@@ -318,7 +319,9 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         for (int j = 0; j < 2; ++j) {
                             uint32_t hi, lo;
                             if (E4M3) {
-                                ph[nt][j] = turned(pack_f16x2(e[nt][2 * j] * fv[j], e[nt][2 * j + 1] * fv[j]));
+                                const float x = e[nt][2 * j] * fv[j], y = e[nt][2 * j + 1] * fv[j];
+                                classes |= below_f16(x) || below_f16(y);
+                                ph[nt][j] = turned(pack_f16x2(x, y));
                             } else {
                                 split_weights(e[nt][2 * j], e[nt][2 * j + 1], hi, lo);
                                 ph[nt][j] = turned(hi); pl[nt][j] = turned(lo);
@@ -382,7 +385,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             expand_alternate(r[0], a[0], a[1]); expand_alternate(r[2], a[2], a[3]);      // piece pc: even channels, odd channels
                             expand_alternate(r[1], b[0], b[1]); expand_alternate(r[3], b[2], b[3]);
                         };
-                        if (!classes) {
+                        if (!__any_sync(0xffffffffu, classes)) {
 #pragma unroll
                             for (int pc = 0; pc < 8; pc += 2) {
                                 uint32_t a[4], b[4];
@@ -394,23 +397,33 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                                 }
                             }
                         } else {
-                            // tokens by classes of exponents, each with a reference of its own; a row of NaN (255) is seen by those whose weight is not 0
-                            bool todo[2] = {t0 + g < m.len, t0 + g + 8 < m.len};
+                            // weights by classes of exponents, each scaled into fp16's normal range; a row of NaN (255) is seen by those whose weight is not 0
+                            const float gv[2] = {ev[0] == 255 && fv[0] != 0.f ? __uint_as_float(0x7fc00000u) : fv[0], ev[1] == 255 && fv[1] != 0.f ? __uint_as_float(0x7fc00000u) : fv[1]};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) e[nt][j] = e[nt][j] == 0.f ? 0.f : e[nt][j] * gv[j >> 1];
                             for (;;) {
-                                const int top = __reduce_max_sync(0xffffffffu, max(todo[0] ? ev[0] : -1, todo[1] ? ev[1] : -1));
-                                if (top < 0) break;
-                                const float back = top == 255 ? 1.f : pow2i(top - e_ref);
+                                uint32_t big = 0;
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) big = max(big, __float_as_uint(e[nt][j]) & 0x7fffffffu);
+                                const int top = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);       // biased exponent of the largest; 255: NaN
+                                if (top == 0) break;
+                                const int up = top == 255 ? 0 : min(141 - top, 126), last = top == 255 ? 255 : top - 28;     // (into [2^14, 2^15); down to 2^-14)
+                                const float f = pow2i(up), back = pow2i(-up);
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                                     for (int j = 0; j < 2; ++j) {
-                                        const bool in = todo[j] && ev[j] > top - 10 && (top < 255 || ev[j] == 255);
-                                        const float f = top == 255 ? __uint_as_float(0x7fc00000u) : pow2i(ev[j] - top);
-                                        const float x = e[nt][2 * j], y = e[nt][2 * j + 1];
-                                        ph[nt][j] = turned(pack_f16x2(in && x != 0.f ? x * f : 0.f, in && y != 0.f ? y * f : 0.f));
+                                        float x = e[nt][2 * j], y = e[nt][2 * j + 1];
+                                        const bool in_x = (int)(__float_as_uint(x) >> 23 & 255u) >= last, in_y = (int)(__float_as_uint(y) >> 23 & 255u) >= last;
+                                        if (in_x) e[nt][2 * j] = 0.f;
+                                        if (in_y) e[nt][2 * j + 1] = 0.f;
+                                        x = in_x ? x * f : 0.f; y = in_y ? y * f : 0.f;
+                                        ph[nt][j] = turned(pack_f16x2(x, y));
                                     }
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) todo[j] &= !(ev[j] > top - 10 && (top < 255 || ev[j] == 255));
 #pragma unroll
                                 for (int pc = 0; pc < 8; pc += 2) {
                                     uint32_t a[4], b[4];
