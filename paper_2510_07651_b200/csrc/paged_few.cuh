@@ -269,7 +269,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         ev[0] = sc[128]; ev[1] = sc[136];
                         // highest exponent of the V rows that the list has (of the finite ones; 1 at least: O's factor 2^(e_ref - 127) has to be a normal number)
                         const bool in0 = t0 + g < m.len, in1 = t0 + g + 8 < m.len;
-                        const int hi = __reduce_max_sync(0xffffffffu, max(in0 && ev[0] < 255 ? ev[0] : 1, in1 && ev[1] < 255 ? ev[1] : 1));
+                        const int hi = __reduce_max_sync(0xffffffffu, max(max(in0 && ev[0] < 255 ? ev[0] : 0, in1 && ev[1] < 255 ? ev[1] : 0), 1));
                         if (e_ref < 0 || hi > e_ref + 4) {          // O follows: P stays below 2^12
                             const float f = e_ref < 0 ? 0.f : pow2i(e_ref - hi);
 #pragma unroll
