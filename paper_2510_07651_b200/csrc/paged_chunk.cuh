@@ -563,8 +563,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::RAWEMPTY + st));
-                    // code bits are the value (finite, whatever the code) times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range; 0 for rows that become zeros
-                    const bool nan = s > 186u, odd = op && nan && t >= c.first_masked && t < seg.m.len, gone = op && (odd || t >= seg.m.len);
+                    // code bits are the value (finite, whatever the code) times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range (so is the product with m1, whose exponent is
+                    // 127 at most: the value times 2^7); 0 for rows that become zeros
+                    const bool nan = s == 255u, odd = op && nan && t >= c.first_masked && t < seg.m.len, gone = op && (odd || t >= seg.m.len);
                     const int e1 = min((int)s - 7, 127), e2 = (int)s - 7 - e1;
                     const __nv_bfloat16 f1 = gone ? __float2bfloat16(0.f) : nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
                     const __nv_bfloat16 f2 = __float2bfloat16(__uint_as_float((uint32_t)(min(e2, 127) + 127) << 23));

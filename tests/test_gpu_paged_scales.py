@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2510_07651_b200 import api
-from tests.paged_helpers import D, Lists, attention_64
+from tests.paged_helpers import D, Lists, attention_64, check
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,17 @@ def test_lists_of_the_smallest_scales(low, T, Hq, H):
     # weights within 2^-8 (sum p v is at most 448 * 2^(low - 127)), o's own rounding, and the steps named above
     ref = attention_64(q, L)[0]
     assert ((o.double() - ref).abs() <= 3 * 2.0 ** -8 * ref.abs() + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("T,Hq,H", SHAPES)
+@pytest.mark.parametrize("up", [63, 80, 105])
+def test_rows_of_large_scales(up, T, Hq, H):
+    """Rows of K and V far beyond 2^60, and queries as small, so that logits are ordinary: scale bytes from 180 to 230."""
+    n = 300
+    g = torch.Generator().manual_seed(up)
+    k, v = torch.randn((1, H, n, D), generator=g) * 2.0 ** up, torch.randn((1, H, n, D), generator=g) * 2.0 ** up
+    L = Lists([n], H, 16, "e4m3", seed=6, k=k, v=v)
+    assert int(L.cache.k_scale[L.cache.table[0, 0].long()].min()) > 110 + up
+    q = (torch.randn((1, Hq, T, D), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda") * 2.0 ** -up).bfloat16()
+    o, lse = api.obc_paged_attention(q, L.cache)
+    check(o, lse, q, L, weight_bits=8)
