@@ -62,6 +62,8 @@ __device__ __forceinline__ void expand(uint32_t x, uint32_t& lo, uint32_t& hi) {
     lo = (x << 4) & 0xf0f0f0f0u;
     hi = (x & 0x80808080u) | ((x >> 4) & 0x07070707u);
 }
+// codes that stand for NaN (all bits but the sign set): the top bit of their bytes
+__device__ __forceinline__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // infinity or NaN in either half
 __device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0x7f80u) == 0x7f80u || (bf16x2 & 0x7f800000u) == 0x7f800000u; }
 // natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)

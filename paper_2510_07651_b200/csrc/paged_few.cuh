@@ -19,6 +19,7 @@
 // takes nearly all of the weight, with a row of V near 0, o consists of such weights.
 #pragma once
 #include "paged_common.cuh"
+#include <cuda_fp16.h>
 #include "tc_ptx.cuh"
 #include "warp_mma.cuh"
 
@@ -278,8 +279,10 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                                 for (int j = 0; j < 8; ++j) { o[nt][j][0] *= f; o[nt][j][1] *= f; o[nt][j][2] *= f; o[nt][j][3] *= f; }
                             e_ref = hi;
                         }
-                        classes = (in0 && ev[0] == 255) || (in1 && ev[1] == 255);
                         fv[0] = in0 ? pow2i(ev[0] - e_ref) : 0.f; fv[1] = in1 ? pow2i(ev[1] - e_ref) : 0.f;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (ev[j] == 255 && fv[j] != 0.f) fv[j] = __uint_as_float(0x7fc00000u);
                     }
                     uint32_t ph[NT][2], pl[NT][2];                  // P^T as B operands: high and low parts
                     float e[NT][4];
@@ -368,20 +371,33 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                             __syncwarp();
                         }
                     }
-                    if (E4M3 && t0 + 16 > m.len) {                  // rows behind the list's end may hold codes that stand for NaN
-                        const int row = tok0 + (lane >> 1);
-                        if (t0 + (lane >> 1) >= m.len) {
+                    unsigned odd = 0;                               // tokens that not every query sees and whose rows hold NaN
+                    if (E4M3 && edge) {                             // rows behind the list's end may hold codes that stand for NaN
+                        const int row = tok0 + (lane >> 1), t = t0 + (lane >> 1);
+                        uint4* at = reinterpret_cast<uint4*>(sv + row * 128 + (lane & 1) * 64);
+                        uint32_t any = 0;
+                        if (t >= m.len) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(sv + row * 128 + (lane & 1) * 64 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            for (int j = 0; j < 4; ++j) at[j] = make_uint4(0u, 0u, 0u, 0u);
+                        } else if (t >= first_masked) {
+                            any = smem[L::kScales + s_at * 256 + 128 + row] == 255 ? 1u : 0u;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint4 u = at[j];
+                                any |= nan_codes(u.x) | nan_codes(u.y) | nan_codes(u.z) | nan_codes(u.w);
+                            }
                         }
-                        fence_async_smem();
                         __syncwarp();
+                        odd = __ballot_sync(0xffffffffu, any != 0u);
+                        odd = (odd | odd >> 1) & 0x55555555u;       // bit 2 i: token i
+                        classes |= odd != 0u;
                     }
                     const int v_row = tok0 + (lane & 7) + (lane >> 4) * 8, v_pc = (lane >> 3) & 1;   // (tokens 0-7, p), (0-7, p + 1), (8-15, p), (8-15, p + 1)
                     if (E4M3) {
-                        auto v_pieces = [&](int pc, uint32_t (&a)[4], uint32_t (&b)[4]) {
+                        auto v_pieces = [&](int pc, uint32_t lo, uint32_t hi, uint32_t (&a)[4], uint32_t (&b)[4]) {      // lo, hi: bytes of the tokens 2 c, + 1 and + 8, + 9 to be taken
                             uint32_t r[4];
                             ldsm_x4_trans(r, sv + v_row * 128 + (((pc + v_pc) ^ (v_row & 7)) << 4));
+                            r[0] &= lo; r[1] &= lo; r[2] &= hi; r[3] &= hi;
                             expand_alternate(r[0], a[0], a[1]); expand_alternate(r[2], a[2], a[3]);      // piece pc: even channels, odd channels
                             expand_alternate(r[1], b[0], b[1]); expand_alternate(r[3], b[2], b[3]);
                         };
@@ -389,7 +405,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
 #pragma unroll
                             for (int pc = 0; pc < 8; pc += 2) {
                                 uint32_t a[4], b[4];
-                                v_pieces(pc, a, b);
+                                v_pieces(pc, ~0u, ~0u, a, b);
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt) {
                                     mma_f16(o[nt][pc], a, ph[nt][0], ph[nt][1]);
@@ -397,20 +413,33 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                                 }
                             }
                         } else {
-                            // weights by classes of exponents, each scaled into fp16's normal range; a row of NaN (255) is seen by those whose weight is not 0
-                            const float gv[2] = {ev[0] == 255 && fv[0] != 0.f ? __uint_as_float(0x7fc00000u) : fv[0], ev[1] == 255 && fv[1] != 0.f ? __uint_as_float(0x7fc00000u) : fv[1]};
+                            // Weights by classes of exponents, each scaled into fp16's normal range.  First all tokens but the odd ones, whose NaN would reach queries of weight 0;
+                            // then those one by one, for the queries that see them.
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) e[nt][j] = e[nt][j] == 0.f ? 0.f : e[nt][j] * gv[j >> 1];
+                                for (int j = 0; j < 4; ++j) e[nt][j] *= fv[j >> 1];
+                            unsigned now = 0x55555555u & ~odd;
+                            bool once = true;
+                            int alone = -1;                         // the one token of the pass
                             for (;;) {
                                 uint32_t big = 0;
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                                    for (int j = 0; j < 4; ++j) big = max(big, __float_as_uint(e[nt][j]) & 0x7fffffffu);
+                                    for (int j = 0; j < 4; ++j)
+                                        if (now >> (2 * g + 16 * (j >> 1)) & 1u) big = max(big, __float_as_uint(e[nt][j]) & 0x7fffffffu);
                                 const int top = (int)(__reduce_max_sync(0xffffffffu, big) >> 23);       // biased exponent of the largest; 255: NaN
-                                if (top == 0) break;
+                                if (top == 0 && !once) {            // (a NaN counts whatever its weight: one pass is there in any case)
+                                    if (!odd) break;
+                                    now = odd & (0u - odd); odd ^= now;
+                                    alone = t0 + ((__ffs(now) - 1) >> 1);
+                                    once = true;
+                                    continue;
+                                }
+                                once = false;
+                                auto bytes = [&](int at) { const unsigned two = now >> at; return (two & 1u ? 0xffffu : 0u) | (two & 4u ? 0xffff0000u : 0u); };
+                                const uint32_t lo = bytes(4 * c), hi = bytes(4 * c + 16);
                                 const int up = top == 255 ? 0 : min(141 - top, 126), last = top == 255 ? 255 : top - 28;     // (into [2^14, 2^15); down to 2^-14)
                                 const float f = pow2i(up), back = pow2i(-up);
 #pragma unroll
@@ -418,7 +447,8 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
 #pragma unroll
                                     for (int j = 0; j < 2; ++j) {
                                         float x = e[nt][2 * j], y = e[nt][2 * j + 1];
-                                        const bool in_x = (int)(__float_as_uint(x) >> 23 & 255u) >= last, in_y = (int)(__float_as_uint(y) >> 23 & 255u) >= last;
+                                        const bool mine_now = now >> (2 * g + 16 * j) & 1u;
+                                        const bool in_x = mine_now && (int)(__float_as_uint(x) >> 23 & 255u) >= last, in_y = mine_now && (int)(__float_as_uint(y) >> 23 & 255u) >= last;
                                         if (in_x) e[nt][2 * j] = 0.f;
                                         if (in_y) e[nt][2 * j + 1] = 0.f;
                                         x = in_x ? x * f : 0.f; y = in_y ? y * f : 0.f;
@@ -427,14 +457,15 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
 #pragma unroll
                                 for (int pc = 0; pc < 8; pc += 2) {
                                     uint32_t a[4], b[4];
-                                    v_pieces(pc, a, b);
+                                    v_pieces(pc, lo, hi, a, b);
 #pragma unroll
                                     for (int nt = 0; nt < NT; ++nt) {
                                         float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
                                         mma_f16(x, a, ph[nt][0], ph[nt][1]);
                                         mma_f16(y, b, ph[nt][0], ph[nt][1]);
 #pragma unroll
-                                        for (int j = 0; j < 4; ++j) { o[nt][pc][j] = fmaf(x[j], back, o[nt][pc][j]); o[nt][pc + 1][j] = fmaf(y[j], back, o[nt][pc + 1][j]); }
+                                        for (int j = 0; j < 4; ++j)
+                                            if (alone < seen[nt][j & 1]) { o[nt][pc][j] = fmaf(x[j], back, o[nt][pc][j]); o[nt][pc + 1][j] = fmaf(y[j], back, o[nt][pc + 1][j]); }
                                     }
                                 }
                             }
@@ -453,7 +484,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         }
                     }
                 }
-                if (edge && !E4M3) fence_async_smem();              // this thread's writes to the stage precede the bulk copy into it
+                if (edge) fence_async_smem();              // this thread's writes to the stage precede the bulk copy into it
                 __syncwarp();
                 if (lane == 0) mbar_arrive(empty(s_at));
             }
