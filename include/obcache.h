@@ -347,7 +347,7 @@ obc_status obc_decode_step(const obc_decode_params* p, obc_tensor q_t, obc_tenso
  *   types   fp32, bf16, or e4m3 with a scale per row: x = code * 2^(scale - 127).  obc_paged_write takes the smallest
  *           power of two for which max |x| <= 448 scales (never below 2^-126; the division is then exact and every
  *           value is rounded once, to nearest, ties to even).  A row that holds an infinity or a NaN is stored with
- *           scale 255 and reads as NaN.
+ *           scale 255 and reads as NaN.  In pages that the caller filled, a code of NaN (0x7f, 0xff) is NaN in its channel.
  *   bounds  lengths and page numbers are read on the device only.  A length counts as if clamped to
  *           [0, max_pages * page_size].  A page number outside [0, n_pages) reads as rows of zeros and is never
  *           written.  Rows of a page behind a list's end may hold anything, NaN among it, and stay as they are.

@@ -84,15 +84,27 @@ __device__ __forceinline__ void store32(void* p, uint32_t a, uint32_t b, uint32_
 }
 template <int N> __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// four bytes (e4m3 codes) -> two bf16 pairs, times m1 * m2 (powers of two that leave the product exact)
-__device__ __forceinline__ void codes_to_bf16(uint32_t x, __nv_bfloat162 m1, __nv_bfloat162 m2, bool two, uint32_t& p01, uint32_t& p23) {
-    uint32_t lo, hi;
-    expand(x, lo, hi);
-    const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
-    __nv_bfloat162 u = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), m1), v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), m1);
-    if (two) { u = __hmul2(u, m2); v = __hmul2(v, m2); }
-    p01 = *reinterpret_cast<const uint32_t*>(&u); p23 = *reinterpret_cast<const uint32_t*>(&v);
+// Four bytes (e4m3 codes) -> two bf16 pairs times m (a power of two).  Through fp16 and fp32, of which a code's values need the upper half alone: the
+// hardware's conversion knows NaN.
+__device__ __forceinline__ void codes_to_bf16(uint32_t x, __nv_bfloat162 m, uint32_t& p01, uint32_t& p23) {
+    uint32_t h[2];
+    expand_adjacent(x, h[0], h[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        const uint32_t b = __byte_perm(__float_as_uint(f.x), __float_as_uint(f.y), 0x7632);
+        const __nv_bfloat162 u = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), m);
+        (i ? p23 : p01) = *reinterpret_cast<const uint32_t*>(&u);
+    }
 }
+
+// 16 bytes of shared memory
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+    uint4 u;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at) : "memory");
+    return u;
+}
+__device__ __forceinline__ void sts16(uint32_t at, uint4 u) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory"); }
 
 template <bool E4M3>
 __global__ void __launch_bounds__(ChunkLayout<E4M3>::kThreads, 1)
@@ -463,7 +475,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                     tc_ld1(tS + (j >> 1), two);
                                     wt = __uint_as_float(j & 1 ? two & 0xffff0000u : two << 16);
                                 }
-                                const int t = t0 + j, page = E4M3 ? -1 : p.c.page_of(m.b, m.h, t);
+                                const int t = t0 + j, page = p.c.page_of(m.b, m.h, t), at_slot = p.c.by_P.mod(t);
+                                const long long at_row = page * p.c.v.sb + m.h * p.c.v.sh + at_slot * p.c.v.st;
+                                float sv = 1.f;
+                                if (E4M3) sv = scale_of(p.c.vs[page * p.c.ss_p + m.h * p.c.ss_h + at_slot]);
 #pragma unroll 1
                                 for (int q = 0; q < 8; ++q) {
                                     uint32_t ov[16];
@@ -472,9 +487,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                                                  "+r"(ov[8]), "+r"(ov[9]), "+r"(ov[10]), "+r"(ov[11]), "+r"(ov[12]), "+r"(ov[13]), "+r"(ov[14]), "+r"(ov[15]) :: "memory");
 #pragma unroll
                                     for (int x = 0; x < 16; ++x) {
-                                        float v = __uint_as_float(0x7fc00000u);                  // (8 bits: a scale that stands for NaN)
-                                        if (!E4M3)
-                                            v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.c.v.ptr)[page * p.c.v.sb + m.h * p.c.v.sh + p.c.by_P.mod(t) * p.c.v.st + q * 16 + x]);
+                                        float v;
+                                        if constexpr (E4M3) {
+                                            uint32_t two, none;
+                                            expand_adjacent(static_cast<const uint8_t*>(p.c.v.ptr)[at_row + q * 16 + x], two, none);
+                                            v = __low2float(*reinterpret_cast<const __half2*>(&two)) * sv;
+                                        } else {
+                                            v = __bfloat162float(static_cast<const __nv_bfloat16*>(p.c.v.ptr)[at_row + q * 16 + x]);
+                                        }
                                         if (j < nvis) ov[x] = __float_as_uint(fmaf(wt, v, __uint_as_float(ov[x])));
                                     }
                                     tc_st16(tO + q * 16, ov);
@@ -553,32 +573,39 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 for (int op = 0; op < 2; ++op, ++n) {
                     const uint32_t st = n & 1, slot = n % NS;
                     if (!all_wait(L::RAWFULL + st, n >> 1, __LINE__)) break;
-                    const uint8_t* raw = smem + L::kRawAt + st * 16384u + row * 128;
+                    const uint32_t raw = sbase + L::kRawAt + st * 16384u + row * 128 + (sw << 4);      // (a row begins on a 128-byte boundary: its pieces' places differ by exclusive or)
                     uint4 x[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint4*>(raw + ((j ^ sw) << 4));
-                    const uint32_t s = smem[L::kScales + st * 128u + row];
+                    for (int j = 0; j < 8; ++j) x[j] = lds16(raw ^ (j << 4));
+                    uint32_t s = smem[L::kScales + st * 128u + row];
                     // (the loads above may still be under way, and nothing below uses them soon: without the fence the bulk copy that the
                     // arrival lets go has been seen to overtake them)
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::RAWEMPTY + st));
-                    // code bits are the value (finite, whatever the code) times 2^-120; 2^(s - 7) = m1 m2, each within bf16's range (so is the product with m1, whose exponent is
-                    // 127 at most: the value times 2^7); 0 for rows that become zeros
-                    const bool nan = s == 255u, odd = op && nan && t >= c.first_masked && t < seg.m.len, gone = op && (odd || t >= seg.m.len);
-                    const int e1 = min((int)s - 7, 127), e2 = (int)s - 7 - e1;
-                    const __nv_bfloat16 f1 = gone ? __float2bfloat16(0.f) : nan ? __float2bfloat16(__uint_as_float(0x7fc00000u)) : __float2bfloat16(__uint_as_float((uint32_t)(e1 + 127) << 23));
-                    const __nv_bfloat16 f2 = __float2bfloat16(__uint_as_float((uint32_t)(min(e2, 127) + 127) << 23));
-                    const __nv_bfloat162 m1 = __halves2bfloat162(f1, f1), m2 = __halves2bfloat162(f2, f2);
+                    // rows of V that not every query sees and that hold NaN become zeros here and are added by hand; so do rows behind the list's end
+                    bool odd = false;
+                    if (op && is_edge(c, (seg.ta + i) * kTokTile)) {
+                        uint32_t codes = s == 255u ? 1u : 0u;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) codes |= nan_codes(x[j].x) | nan_codes(x[j].y) | nan_codes(x[j].z) | nan_codes(x[j].w);
+                        odd = codes != 0u && t >= c.first_masked && t < seg.m.len;
+                        if (odd || t >= seg.m.len) {
+                            s = 0;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = make_uint4(0u, 0u, 0u, 0u);
+                        }
+                    }
+                    const __nv_bfloat16 f = __float2bfloat16(scale_of(s));
+                    const __nv_bfloat162 m = __halves2bfloat162(f, f);
                     if (!all_wait(L::EMPTY + slot, (n / NS) ^ 1u, __LINE__)) break;
-                    uint8_t* dst = smem + L::kRing + slot * kOperandBytes + row * 128;
-                    const bool two = __any_sync(0xffffffffu, e2 > 0);
+                    const uint32_t dst = sbase + L::kRing + slot * kOperandBytes + row * 128 + (sw << 4);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {                  // 8 channels at a time
                         uint4 y;
-                        codes_to_bf16(j & 1 ? x[j >> 1].z : x[j >> 1].x, m1, m2, two, y.x, y.y);
-                        codes_to_bf16(j & 1 ? x[j >> 1].w : x[j >> 1].y, m1, m2, two, y.z, y.w);
-                        *reinterpret_cast<uint4*>(dst + (j >> 3) * kHalfBytes + (((j & 7) ^ sw) << 4)) = y;
+                        codes_to_bf16(j & 1 ? x[j >> 1].z : x[j >> 1].x, m, y.x, y.y);
+                        codes_to_bf16(j & 1 ? x[j >> 1].w : x[j >> 1].y, m, y.z, y.w);
+                        sts16((dst ^ ((j & 7) << 4)) + (j >> 3) * kHalfBytes, y);
                     }
                     const uint32_t word = __ballot_sync(0xffffffffu, odd);
                     if (op && lane == 0) bad_words[slot * 4 + (warp - 12)] = word;

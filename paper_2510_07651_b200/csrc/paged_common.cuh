@@ -10,6 +10,7 @@
 // and its last, and an item that is shared is the last one of the CTA that it begins in: the merge goes by these CTAs.
 #pragma once
 #include "obc_common.cuh"
+#include <cuda_fp16.h>
 
 namespace obc {
 namespace {
@@ -56,12 +57,12 @@ __device__ __forceinline__ int seen_by(const AttnParams& p, const Item& m, int r
     return p.causal ? min(max(m.len - m.ql + p.by_G.div(m.r0 + r) + 1, 0), m.len) : m.len;
 }
 
-// four e4m3 codes as the low and the high bytes of bf16 numbers: their bits, shifted into bf16's fields, stand for the value times 2^-120
-// (subnormal codes included)
-__device__ __forceinline__ void expand(uint32_t x, uint32_t& lo, uint32_t& hi) {
-    lo = (x << 4) & 0xf0f0f0f0u;
-    hi = (x & 0x80808080u) | ((x >> 4) & 0x07070707u);
+// four e4m3 codes as fp16 pairs: (b0, b1) and (b2, b3)
+__device__ __forceinline__ void expand_adjacent(uint32_t x, uint32_t& p01, uint32_t& p23) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(p01), "=r"(p23) : "r"(x));
 }
+// a row's scale from its byte
+__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s == 0u ? 0x00400000u : s << 23); }
 // codes that stand for NaN (all bits but the sign set): the top bit of their bytes
 __device__ __forceinline__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // infinity or NaN in either half

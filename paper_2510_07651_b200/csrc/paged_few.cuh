@@ -19,7 +19,6 @@
 // takes nearly all of the weight, with a row of V near 0, o consists of such weights.
 #pragma once
 #include "paged_common.cuh"
-#include <cuda_fp16.h>
 #include "tc_ptx.cuh"
 #include "warp_mma.cuh"
 
@@ -40,10 +39,7 @@ template <int NT, bool E4M3> struct FewLayout {
     static constexpr uint32_t kSmem = kBars + (kFull + kStages) * 8u + 1024;               // + alignment slack
 };
 
-// four e4m3 codes as fp16 pairs: (b0, b1) and (b2, b3), or (b0, b2) and (b1, b3)
-__device__ __forceinline__ void expand_adjacent(uint32_t x, uint32_t& p01, uint32_t& p23) {
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(p01), "=r"(p23) : "r"(x));
-}
+// (b0, b2) and (b1, b3)
 __device__ __forceinline__ void expand_alternate(uint32_t x, uint32_t& p02, uint32_t& p13) { expand_adjacent(__byte_perm(x, 0u, 0x3120), p02, p13); }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
@@ -58,8 +54,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
 __device__ __forceinline__ bool below_f16(float x) { return __float_as_uint(x) - 1u < 0x387fffffu; }
 // 2^e for whole e (0 and infinity beyond fp32's exponents)
 __device__ __forceinline__ float pow2i(int e) { return e < -126 ? 0.f : e > 127 ? INFINITY : __uint_as_float((uint32_t)(e + 127) << 23); }
-// a row's scale from its byte
-__device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s == 0u ? 0x00400000u : s << 23); }
 
 // B operands of all steps from one row of q (nullptr: zeros): channels 16 ks + 2 c, + 1 and + 8, + 9.  e4m3: 16 ks + 4 c, .. + 3 as fp16 times a
 // power of two; the result is what undoes it.  The four lanes of a row call together.

@@ -10,7 +10,7 @@ from tests.paged_helpers import D, Lists, check
 
 pytestmark = pytest.mark.gpu
 
-SHAPES = [(1, 8, 2), (1, 16, 1), (4, 4, 2), (4, 8, 2)]      # T, Hq, Hkv: up to 8 and to 16 rows per list
+SHAPES = [(1, 8, 2), (1, 16, 1), (4, 4, 2), (4, 8, 2), (40, 4, 2), (130, 4, 2)]      # T, Hq, Hkv: up to 8 and to 16 rows per list, and more
 
 
 def _codes(L, name, h, t):
