@@ -401,7 +401,7 @@ obc_status obc_paged_read(const obc_pages* c, int32_t n_tokens, obc_tensor k_out
  *   q, o   [B,Hq,n_tokens,d], one type: f32 over f32 pages, bf16 over bf16 or e4m3 pages
  *   lse    device fp32 [B,Hq,n_tokens] contiguous, or NULL
  * Rows i >= q_len of o and lse are left as they are.  Sums and softmax statistics are fp32.  Infinities and NaN are no
- * different from any value in a row that a query sees, and reach no query that does not see them.
+ * different from any value in a row that a query sees, and reach no query that does not see them (a logit of +inf makes lse +inf and o NaN).
  * The work is counted in tiles of 128 tokens and of 256 (8 or 16 where a list has no more) rows, in 32 bits over all lists at their longest
  * (max_pages * page_size): what exceeds that is refused (OBC_ERR_SHAPE).
  * A device-side wait that gives up raises the workspace's status word: obc_score_status() reads it.

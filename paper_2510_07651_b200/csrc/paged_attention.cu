@@ -33,12 +33,12 @@ paged_merge_kernel(const __grid_constant__ AttnParams p) {
     float top = -INFINITY;
     for (int s = lane; s < n; s += 32) top = fmaxf(top, p.part_m[at(s)]);
     top = warp_max(top);
-    const float ref = top == -INFINITY ? 0.f : top;
+    const float ref = reference(top);
     float total = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s0 = 0; s0 < n; s0 += 32) {
         const int s = s0 + lane, cnt = min(32, n - s0);
-        const float w = s < n ? exp2f(p.part_m[at(s)] - ref) : 0.f;
+        const float w = s < n ? share_of(p.part_m[at(s)], ref) : 0.f;
         if (s < n) total = fmaf(w, p.part_l[at(s)], total);
 #pragma unroll 8
         for (int j = 0; j < cnt; ++j) {
@@ -142,7 +142,7 @@ paged_f32_kernel(const __grid_constant__ AttnParams p) {
                     float* row = sS + (r0 + j) * kF32Tok;
                     const float a = lane < n[j] ? row[lane] : -INFINITY, b = lane + 32 < n[j] ? row[lane + 32] : -INFINITY;
                     const float top = fmaxf(warp_max(fmaxf(a, b)), mx[j]);
-                    const float ref = top == -INFINITY ? 0.f : top, f = exp2f(mx[j] - ref);
+                    const float ref = reference(top), f = share_of(mx[j], ref);
                     const float ea = exp2f(a - ref), eb = exp2f(b - ref);
                     l[j] = fmaf(l[j], f, ea + eb);                      // per lane; joined at the end
                     acc[j].x *= f; acc[j].y *= f; acc[j].z *= f; acc[j].w *= f;
@@ -166,7 +166,7 @@ paged_f32_kernel(const __grid_constant__ AttnParams p) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int r = r0 + j;
-            const float total = warp_sum(l[j]), ref = mx[j] == -INFINITY ? 0.f : mx[j];
+            const float total = warp_sum(l[j]), ref = reference(mx[j]);
             if (r >= m.rows) continue;
             if (seg.whole()) {
                 const float inv = total != 0.f ? 1.f / total : 0.f;

@@ -431,7 +431,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         l *= factor;
                         if (need) m_used = mt;
                     }
-                    const float m_eff = m_used == -INFINITY ? 0.f : m_used;
+                    const float m_eff = reference(m_used);
                     const float2 negm = make_float2(-m_eff, -m_eff);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -554,7 +554,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                 }
             }
-            if (there && whole && p.lse) p.lse[lse_at] = lse_of(m_used == -INFINITY ? 0.f : m_used, l);
+            if (there && whole && p.lse) p.lse[lse_at] = lse_of(reference(m_used), l);
             if (there && !whole) { p.part_m[at] = m_used; p.part_l[at] = l; }
             tc_fence_before();                                      // (O is read: the next segment's MMAs follow the next P's barrier)
             if (next_q) q_there();

@@ -67,6 +67,11 @@ __device__ __forceinline__ float scale_of(uint32_t s) { return __uint_as_float(s
 __device__ __forceinline__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 // infinity or NaN in either half
 __device__ __forceinline__ bool not_finite(uint32_t bf16x2) { return (bf16x2 & 0x7f80u) == 0x7f80u || (bf16x2 & 0x7f800000u) == 0x7f800000u; }
+// The maximum that logits are taken relative to, kept finite: with infinite logits sums become infinite or NaN as they should, where a difference of two infinities
+// would be NaN always; and if all are -inf their weights are 0.
+__device__ __forceinline__ float reference(float top) { return fminf(fmaxf(top, -3.402823466e38f), 3.402823466e38f); }
+// what sums relative to `top` count for relative to the reference of a maximum that is no smaller
+__device__ __forceinline__ float share_of(float top, float ref) { return exp2f(fminf(top, 3.402823466e38f) - ref); }
 // natural log-sum-exp from the reference in log2 units and the sum above it; a row that saw nothing has sum 0 (and log2(0) = -inf)
 __device__ __forceinline__ float lse_of(float ref, float total) { return (ref + log2f(total)) * 0.6931471805599453f; }
 

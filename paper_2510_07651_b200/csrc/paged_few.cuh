@@ -307,8 +307,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const float ref = mx[nt][j & 1];
-                            const float x = fast_exp2(s[nt][j] - (ref == -INFINITY ? 0.f : ref));
+                            const float x = fast_exp2(s[nt][j] - reference(mx[nt][j & 1]));
                             l[nt][j & 1] += x;
                             e[nt][j] = x;
                         }
@@ -503,10 +502,10 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                 float top = -INFINITY;
 #pragma unroll
                 for (int w = 0; w < L::kWarps; ++w) top = fmaxf(top, sm[w * ROWS + r]);
-                ref = top == -INFINITY ? 0.f : top;
+                ref = reference(top);
                 total = 0.f;
 #pragma unroll
-                for (int w = 0; w < L::kWarps; ++w) total = fmaf(exp2f(sm[w * ROWS + r] - ref), sl[w * ROWS + r], total);
+                for (int w = 0; w < L::kWarps; ++w) total = fmaf(share_of(sm[w * ROWS + r], ref), sl[w * ROWS + r], total);
             };
             float f[NT][2], ref_w[NT], sum_w[NT];                   // factors of the lane's rows; statistics of row 8 nt + wg
 #pragma unroll
@@ -516,7 +515,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
                     float top = -INFINITY;
 #pragma unroll
                     for (int w = 0; w < L::kWarps; ++w) top = fmaxf(top, sm[w * ROWS + nt * 8 + 2 * c + j]);
-                    f[nt][j] = exp2f(mx[nt][j] - (top == -INFINITY ? 0.f : top)) * (E4M3 ? (e_ref < 0 ? 1.f : pow2i(e_ref - 127)) : 1.f);
+                    f[nt][j] = share_of(mx[nt][j], reference(top)) * (E4M3 ? (e_ref < 0 ? 1.f : pow2i(e_ref - 127)) : 1.f);
                 }
                 joined(nt * 8 + wg, ref_w[nt], sum_w[nt]);
             }
