@@ -458,21 +458,25 @@ def evict_to_pages(q, k, v, cache: PagedCache, *, budget, seq_lens=None, variant
     [B,Hkv], contiguous (a head may keep as many tokens as its list's pages hold).  A sequence that the selection cannot serve (shorter than
     the budget, or a head that would keep more than its list holds: rows of -1 in idx) leaves empty lists.  Returns (idx, scores)."""
     n_recent = q.shape[2] if n_recent is None else n_recent
+    if any(n > 1 and s == 0 for n, s in zip(cache.lens.shape, cache.lens.stride())):
+        raise ValueError("the lengths of a cache that is written must not share memory")
     scores = obc_score(q, k, v, seq_lens=seq_lens, causal=causal, variants=(variant,), path=path)
     room = cache.table.shape[-1] * cache.k.shape[2]
+    lens = torch.empty_like(cache.lens)                        # (cache.lens is set when the write has been accepted: a refused call leaves it as it was)
     if safeguard is None:
         if budget > room:
             raise ValueError("the lists' pages do not hold the budget")
         idx = obc_select(scores[0], budget=budget, seq_lens=seq_lens, n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel)
-        cache.lens.fill_(budget)
+        lens.fill_(budget)
         if seq_lens is not None:
-            cache.lens.mul_((seq_lens >= budget).view(-1, *[1] * (cache.lens.dim() - 1)))
-        obc_paged_write(cache, k, v, idx=idx)
+            lens.mul_((seq_lens >= budget).view(-1, *[1] * (lens.dim() - 1)))
+        obc_paged_write(cache._replace(lens=lens), k, v, idx=idx)
     else:
         if cache.lens.dim() != 2 or not cache.lens.is_contiguous() or (cache.table.dim() != 3 and cache.k.shape[1] > 1):
             raise ValueError("head-adaptive budgets need a list per head: lens [B,Hkv], table [B,Hkv,max_pages]")
         idx, _ = obc_select_adaptive(scores[0], budget=budget, safeguard=safeguard, idx_stride=min(room, k.shape[2]), seq_lens=seq_lens,
-                                     n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel, counts=cache.lens)
-        cache.lens.clamp_(min=0)
-        obc_paged_write(cache, k, v, new_lens=cache.lens, idx=idx)
+                                     n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel, counts=lens)
+        lens.clamp_(min=0)
+        obc_paged_write(cache._replace(lens=lens), k, v, new_lens=lens, idx=idx)
+    cache.lens.copy_(lens)
     return idx, scores
