@@ -460,20 +460,24 @@ def evict_to_pages(q, k, v, cache: PagedCache, *, budget, seq_lens=None, variant
     n_recent = q.shape[2] if n_recent is None else n_recent
     if any(n > 1 and s == 0 for n, s in zip(cache.lens.shape, cache.lens.stride())):
         raise ValueError("the lengths of a cache that is written must not share memory")
-    scores = obc_score(q, k, v, seq_lens=seq_lens, causal=causal, variants=(variant,), path=path)
     room = cache.table.shape[-1] * cache.k.shape[2]
-    lens = torch.empty_like(cache.lens)                        # (cache.lens is set when the write has been accepted: a refused call leaves it as it was)
     if safeguard is None:
         if budget > room:
             raise ValueError("the lists' pages do not hold the budget")
+    else:
+        if cache.lens.dim() != 2 or not cache.lens.is_contiguous() or (cache.table.dim() != 3 and cache.k.shape[1] > 1):
+            raise ValueError("head-adaptive budgets need a list per head: lens [B,Hkv], table [B,Hkv,max_pages]")
+        if cache.lens.dtype != torch.int32 or cache.lens.shape != k.shape[:2] or cache.lens.device != k.device:
+            raise ValueError("cache.lens, which the selection writes, must be an int32 tensor [B,Hkv] on k's device")
+    scores = obc_score(q, k, v, seq_lens=seq_lens, causal=causal, variants=(variant,), path=path)
+    lens = torch.empty_like(cache.lens)                        # (cache.lens is set when the write has been accepted: a refused call leaves it as it was)
+    if safeguard is None:
         idx = obc_select(scores[0], budget=budget, seq_lens=seq_lens, n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel)
         lens.fill_(budget)
         if seq_lens is not None:
             lens.mul_((seq_lens >= budget).view(-1, *[1] * (lens.dim() - 1)))
         obc_paged_write(cache._replace(lens=lens), k, v, idx=idx)
     else:
-        if cache.lens.dim() != 2 or not cache.lens.is_contiguous() or (cache.table.dim() != 3 and cache.k.shape[1] > 1):
-            raise ValueError("head-adaptive budgets need a list per head: lens [B,Hkv], table [B,Hkv,max_pages]")
         idx, _ = obc_select_adaptive(scores[0], budget=budget, safeguard=safeguard, idx_stride=min(room, k.shape[2]), seq_lens=seq_lens,
                                      n_sink=n_sink, n_recent=n_recent, pool=pool, pool_kernel=pool_kernel, counts=lens)
         lens.clamp_(min=0)
