@@ -397,8 +397,13 @@ def obc_paged_write(cache: PagedCache, k, v, *, new_lens=None, idx=None) -> None
 
 
 def obc_paged_read(cache: PagedCache, *, n_tokens=None, dtype=None, k_out=None, v_out=None):
-    """The lists as dense caches (k, v) [B,Hkv,n_tokens,d], float32 or bfloat16.  Given outputs keep what they hold behind a list's end;
-    outputs made here (n_tokens: default all that the table can hold) hold zeros there."""
+    """The lists as dense caches (k, v) [B,Hkv,n_tokens,d], float32 or bfloat16.  Given outputs keep what they hold behind a list's end, and n_tokens and
+    dtype, if given as well, have to agree with them; outputs made here (n_tokens: default all that the table can hold) hold zeros there."""
+    for out in (k_out, v_out):
+        if out is not None and n_tokens is not None and out.dim() == 4 and out.shape[2] != n_tokens:
+            raise ValueError(f"n_tokens is {n_tokens}, but the output given has room for {out.shape[2]}")
+        if out is not None and dtype is not None and dtype in (torch.float32, torch.bfloat16) and out.dtype != dtype:
+            raise ValueError(f"dtype is {dtype}, but the output given is {out.dtype}")
     if n_tokens is None:
         n_tokens = cache.table.shape[-1] * cache.k.shape[2]
     if dtype is None:
