@@ -74,8 +74,8 @@ __device__ __forceinline__ float q_fragments(uint32_t (&b)[8][2], const __nv_bfl
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = (int)(top >> 7);           // biased exponent; 0: zeros or subnormals, 255: infinity or NaN (the row's result is NaN either way)
-    const int up = e == 255 ? 0 : min(141 - e, 126);      // (2^-up has to be a normal number)
+    const int e = (int)(top >> 7);           // biased exponent; 0: zeros or subnormals, 255: infinity or NaN (beside which finite values only have to stay finite)
+    const int up = e == 255 ? -114 : min(141 - e, 126);   // (2^-up has to be a normal number)
     const float f = pow2i(up);
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
